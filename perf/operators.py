@@ -40,7 +40,7 @@ def listed():
         # one very long document in 8 bits: the work of few heads has to be split over the whole GPU
         _case("decode_one_long_e4m3", "decode", dtype="e4m3", kv_heads=4, group=16, page=32, min_len=200001, max_len=200001),
         # the decode step after an eviction: every head has a table and a length of its own
-        _case("append_decode_small", "append_decode", n_seqs=8, kv_heads=16, min_len=152, max_len=153, per_head=True),
+        _case("append_decode_small", "append_decode", n_seqs=8, kv_heads=16, min_len=152, max_len=153, per_head=True, weights=True),
         # the hires7b step, rows in 8 bits, quantised on the way in
         _case("append_decode_hires_e4m3", "append_decode", dtype="e4m3", n_seqs=16, kv_heads=32, min_len=2500, max_len=4224),
         # the rows of one decode step of the janus7b batch
@@ -212,10 +212,10 @@ def prepare(case, seed):
         x = torch.exp(2.0 * torch.randn((n_seqs, h, max(1, c["max_len"])), generator=g, device="cuda"))
         s["scores"] = torch.where(torch.rand(x.shape, generator=g, device="cuda") < 0.02, torch.zeros_like(x), x)
     if evict:
-        width = max(1, int(kept_need.max()))
-        s["dst_table"] = table(kept_need, total, width)
+        most = min(int(_keep(c).max()), wide * page)          # columns that any of the heads may need
+        s["dst_table"] = table(kept_need, total, -(-most // page))
         s["dst_lengths"] = torch.zeros_like(lens)
-        s["dst_scores"] = torch.zeros((n_seqs, h, max(1, int(kept.max()))), device="cuda")
+        s["dst_scores"] = torch.zeros((n_seqs, h, most), device="cuda")
     if own:
         from paper_2510_18716_b200 import binding
         s["cache"] = binding.PagedKV(s["k"], s["v"], s["table"], s["lengths"], k_scales=s["ks"], v_scales=s["vs"], scores=s["scores"])
@@ -283,7 +283,8 @@ def _plain_attend(s):
 
 
 def _quantize(x):
-    scale = x.abs().amax(dim=-1) / E4M3_MAX
+    top = x.abs().amax(dim=-1)
+    scale = top / torch.full_like(top, E4M3_MAX)              # a true division: by a plain number, torch multiplies by its inverse
     by = torch.where(scale > 0, scale, torch.ones_like(scale))
     return (x / by[..., None]).clamp(-E4M3_MAX, E4M3_MAX).to(torch.float8_e4m3fn), scale
 
@@ -314,6 +315,8 @@ def _plain_append(s):
     at = (page[ok], head[ok], (slot % c["page"])[ok])
     _store(s["k"], s["ks"], at, s["k_new"][ok])
     _store(s["v"], s["vs"], at, s["v_new"][ok])
+    if s["scores"] is not None:                               # a new token has had no weight yet
+        s["scores"][seq[:, None].expand_as(slot)[ok], torch.arange(c["kv_heads"], device="cuda").expand_as(slot)[ok], slot[ok]] = 0.0
     return _cache(s)
 
 
@@ -333,10 +336,10 @@ def _plain_evict(s):
     keep = c["prefix"] + budget + recent
     kept = (slot < n) & ((n <= keep) | ~candidate | (rank < budget))
     new = kept.sum(dim=2)
-    wide = s["dst_scores"].shape[2]
-    src = torch.sort((~kept).to(torch.uint8), dim=2, stable=True).indices[:, :, :wide]
-    to = torch.arange(wide, device="cuda").expand(c["n_seqs"], c["kv_heads"], -1)
+    to = torch.arange(s["dst_scores"].shape[2], device="cuda").expand(c["n_seqs"], c["kv_heads"], -1)
     live = to < new[..., None]
+    first = torch.sort((~kept).to(torch.uint8), dim=2, stable=True).indices
+    src = torch.gather(first, 2, to.clamp(max=first.shape[2] - 1))
     head = _head(s, to)
     a, b = _where(s, src), _where(s, to, "dst_table")
     at, put = (a[0][live], head[live], a[1][live]), (b[0][live], head[live], b[1][live])
@@ -434,6 +437,8 @@ def exact(case, seed):
             out[i, h * group:(h + 1) * group] = (e / z) @ v
             lse[i, h * group:(h + 1) * group] = (top + z.log())[:, 0]
             if scores is not None:
+                if c["op"] == "append_decode":
+                    scores[i, h, m - 1] = 0.0                 # the new token's
                 scores[i, h, :m] += (e / z).sum(dim=0)
     got = {"out": out, "lse": lse, **({"scores": scores} if c["weights"] else {})}
     if c["op"] == "append_decode":
