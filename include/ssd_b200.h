@@ -365,6 +365,116 @@ int64_t ssd_debug_decode_plan(int32_t n_heads, const int32_t *head_recs, int32_t
                               int32_t t_img, int32_t max_workers, int32_t chunk,
                               int64_t *copies_out, int64_t cap);
 
+/* ------------------------------------------------------------------------------------------------
+ * The paged cache: the same two decisions (attend over what is kept; keep what has been attended to)
+ * for serving sequences of different lengths, with query heads that share key heads.
+ *
+ * K and V live in pools of pages; a page holds page_size consecutive tokens ("slots") of every key
+ * head, or of one head (head_stride 0 with a table row per head).  Row r of page g of head h starts
+ * at k_pages + g * page_stride + h * head_stride + r * slot_stride (elements; head_dim consecutive
+ * elements per row), and V's rows lie the same way from v_pages.  Slot s of head h of sequence b is
+ * row s % page_size of the page named by page_table[b * table_seq_stride + h * table_head_stride +
+ * s / page_size] (table_head_stride 0: the heads of a sequence share its pages; entries behind the
+ * last slot are not read).  lengths[b * len_seq_stride + h * len_head_stride] is the number of slots
+ * held (len_head_stride 0: one length per sequence).  8-bit rows (E4M3 codes) have a float32 scale
+ * each: scale = max|x| / 448, code = E4M3(x / scale), as in ssd_cache_set_kv_format.
+ * scores (optional): the attention weights each slot has had so far, float32, row of score_slots
+ * values per (sequence, head).
+ *
+ * The library keeps nothing between calls.  Lengths, tables and scores are device memory, so a
+ * captured call follows them when it is replayed.  Device data is checked by the kernels: a slot
+ * whose page number lies outside [0, n_pages) counts as masked and is never written, a length
+ * outside [0, max_pages * page_size] is cut to that range, and either sets a bit of *status.  What a
+ * call writes (pages of the appended or moved rows, lengths, scores) must not be used by another
+ * stream meanwhile.  Row and table strides are not negative; pages and their strides, q, out and the
+ * new rows are aligned to 16 bytes. */
+enum ssd_paged_dtype { SSD_PAGED_BF16 = 0, SSD_PAGED_FP16 = 1, SSD_PAGED_E4M3 = 2 };
+
+/* bits of the status word of a paged cache (sticky; the caller clears them) */
+enum ssd_paged_status_bit {
+  SSD_PAGED_BAD_PAGE = 1,    /* a page number outside the pool */
+  SSD_PAGED_BAD_LENGTH = 2,  /* a length outside the table, or appended rows that do not fit in it */
+  SSD_PAGED_BAD_SCORES = 4   /* a slot behind the end of its score row: its weight is dropped */
+};
+
+typedef struct ssd_paged_kv {
+  void *k_pages, *v_pages;
+  float *k_scales, *v_scales; /* SSD_PAGED_E4M3 only, else NULL */
+  const int32_t *page_table;
+  int32_t *lengths;
+  float *scores;              /* or NULL */
+  uint32_t *status;           /* device word, or NULL */
+  int64_t page_stride, head_stride, slot_stride;                   /* elements of the pages */
+  int64_t scale_page_stride, scale_head_stride, scale_slot_stride; /* elements of the scales */
+  int64_t table_seq_stride, table_head_stride;
+  int64_t len_seq_stride, len_head_stride;
+  int64_t score_seq_stride, score_head_stride;
+  int32_t dtype;        /* ssd_paged_dtype of the pages */
+  int32_t n_seqs;
+  int32_t n_kv_heads;   /* <= 128 */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t page_size;    /* any, from 1 */
+  int32_t n_pages;      /* of the pool */
+  int32_t max_pages;    /* columns of the table; max_pages * page_size < 2^30 */
+  int32_t score_slots;  /* columns of the scores */
+} ssd_paged_kv;
+
+typedef struct ssd_paged_attn {
+  const void *q;              /* [n_seqs, n_q_heads, head_dim] */
+  void *out;                  /* the same shape and type */
+  const void *k_new, *v_new;  /* ssd_paged_append_decode: [n_seqs, n_kv_heads, head_dim], q's type */
+  float *lse;                 /* [n_seqs, n_q_heads] log of the softmax's sum, -inf where nothing is held; or NULL */
+  void *workspace;            /* ssd_paged_workspace_bytes; 256-byte aligned */
+  size_t workspace_bytes;
+  int64_t q_seq_stride, q_head_stride, out_seq_stride, out_head_stride; /* elements */
+  int64_t new_seq_stride, new_head_stride;
+  int32_t q_dtype;            /* SSD_PAGED_BF16 or SSD_PAGED_FP16; the pages' type where that has 16 bits */
+  int32_t n_q_heads;          /* a multiple of n_kv_heads; query heads h * g .. h * g + g - 1 share key head h */
+  int32_t accumulate;         /* 1: add every slot's weights, summed over the query heads, to the scores */
+  float softmax_scale;        /* 0 selects 1/sqrt(head_dim) */
+} ssd_paged_attn;
+
+/* Bytes of workspace of the two attention calls on the current device (0: bad arguments).  The
+ * workspace must be zero before its first use; every call leaves it ready for the next one.  Calls
+ * that may run at the same time need workspaces of their own (two captured graphs may share one
+ * only if they are never replayed at the same time); caches used in turn on one stream can share. */
+size_t ssd_paged_workspace_bytes(const ssd_paged_kv *kv, int32_t n_q_heads, int32_t accumulate);
+
+/* Appends rows.  lengths already count them: with cu_seqlens NULL, n_tokens = n_seqs and token b is
+ * the newest of sequence b (slot length - 1 of every head); else the tokens cu_seqlens[b] ..
+ * cu_seqlens[b + 1] - 1 (device, n_seqs + 1 ascending values, the last one n_tokens) are the newest
+ * ones of sequence b, in order.  k_new, v_new [n_tokens, n_kv_heads, head_dim] of type new_dtype
+ * (bf16 or fp16; the pages' type where that has 16 bits), with the given strides.  Appended slots
+ * start with a score of zero.  A token that would lie before slot 0 or behind the table is dropped
+ * (SSD_PAGED_BAD_LENGTH); one of a sequence of length 0 with cu_seqlens NULL is dropped silently
+ * (padding of a batch). */
+int ssd_paged_append(const ssd_paged_kv *kv, const void *k_new, const void *v_new, int32_t new_dtype,
+                     int64_t new_token_stride, int64_t new_head_stride, const int32_t *cu_seqlens,
+                     int32_t n_tokens, void *stream);
+
+/* Attention of one new token per sequence over all slots held.  A sequence (or head) that holds
+ * none gets zeros. */
+int ssd_paged_decode_attn(const ssd_paged_kv *kv, const ssd_paged_attn *args, void *stream);
+
+/* ssd_paged_append of one token per sequence, then ssd_paged_decode_attn, in one launch. */
+int ssd_paged_append_decode(const ssd_paged_kv *kv, const ssd_paged_attn *args, void *stream);
+
+/* Eviction by accumulated weight, per (sequence, head) with n slots held: if n <= prefix + budget[h]
+ * + recent[h] all are kept, else slots [0, prefix), the budget[h] slots of [prefix, n - recent[h])
+ * with the highest scores (ties: the lowest slot; a NaN counts as lowest), and the last recent[h].  The
+ * kept tokens move, in order, to slots 0, 1, .. of `into`, with their scores, and into->lengths is
+ * set.  into NULL: in place (pages that other sequences share must not be among those it rewrites:
+ * the ones from the first dropped slot on).  Else `into` names other pages (of the same pool or not;
+ * same type, head_dim, heads and sequences), and the source is left as it was.
+ * budget_host, recent_host: [n_kv_heads], read before the call returns.  With one length per
+ * sequence (len_head_stride 0) budget + recent must be the same for all heads.
+ * kept (device, [n_seqs, n_kv_heads, kept_cols]): the source slot of each kept token, -1 behind the
+ * last one; kept_cols >= min(prefix + max(budget + recent), max_pages * page_size).
+ * counts (device, [n_seqs, n_kv_heads]): how many are kept. */
+int ssd_paged_evict(const ssd_paged_kv *kv, const ssd_paged_kv *into, int32_t prefix,
+                    const int32_t *budget_host, const int32_t *recent_host, int32_t *kept,
+                    int32_t kept_cols, int32_t *counts, void *stream);
+
 /* Number of kernels this library has launched since the process started (for audit). */
 uint64_t ssd_kernel_launch_count(void);
 

@@ -33,6 +33,7 @@ EXPORTS = [
     "ssd_cache_set_row_buffer", "ssd_recompress", "ssd_cache_get_scores", "ssd_append_decode",
     "ssd_labels_from_ratio_sums", "ssd_labels_from_sparsity", "ssd_cache_get_compress_scores", "ssd_kv_token_mse",
     "ssd_cache_set_kv_format", "ssd_quantize_rows_e4m3",
+    "ssd_paged_workspace_bytes", "ssd_paged_append", "ssd_paged_decode_attn", "ssd_paged_append_decode", "ssd_paged_evict",
 ]
 
 
@@ -40,6 +41,20 @@ class SsdConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "n_layers", "n_seqs", "n_heads", "head_dim", "prompt_len", "max_image_tokens", "window",
         "sink_budget", "sink_recent", "cls_window")] + [("tau", C.c_float), ("softmax_scale", C.c_float)]
+
+
+class SsdPagedKv(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scales", "v_scales", "page_table", "lengths", "scores", "status")]
+                + [(n, C.c_int64) for n in (
+                    "page_stride", "head_stride", "slot_stride", "scale_page_stride", "scale_head_stride", "scale_slot_stride",
+                    "table_seq_stride", "table_head_stride", "len_seq_stride", "len_head_stride", "score_seq_stride", "score_head_stride")]
+                + [(n, C.c_int32) for n in ("dtype", "n_seqs", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "score_slots")])
+
+
+class SsdPagedAttn(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "k_new", "v_new", "lse", "workspace")] + [("workspace_bytes", C.c_size_t)]
+                + [(n, C.c_int64) for n in ("q_seq_stride", "q_head_stride", "out_seq_stride", "out_head_stride", "new_seq_stride", "new_head_stride")]
+                + [(n, C.c_int32) for n in ("q_dtype", "n_q_heads", "accumulate")] + [("softmax_scale", C.c_float)])
 
 
 class SsdError(RuntimeError):
@@ -107,6 +122,13 @@ def load():
     L.ssd_cache_device_status.argtypes = [vp, C.POINTER(C.c_uint32)]
     L.ssd_debug_decode_plan.argtypes = [i32, vp, i32, i32, i32, i32, i32, i32, i32, vp, C.c_int64]
     L.ssd_debug_decode_plan.restype = C.c_int64
+    kvp = C.POINTER(SsdPagedKv)
+    L.ssd_paged_workspace_bytes.argtypes = [kvp, i32, i32]
+    L.ssd_paged_workspace_bytes.restype = C.c_size_t
+    L.ssd_paged_append.argtypes = [kvp, vp, vp, i32, C.c_int64, C.c_int64, vp, i32, vp]
+    L.ssd_paged_decode_attn.argtypes = [kvp, C.POINTER(SsdPagedAttn), vp]
+    L.ssd_paged_append_decode.argtypes = [kvp, C.POINTER(SsdPagedAttn), vp]
+    L.ssd_paged_evict.argtypes = [kvp, kvp, i32, vp, vp, vp, i32, vp, vp]
     L.ssd_kernel_launch_count.argtypes = []
     L.ssd_kernel_launch_count.restype = u64
     for n in EXPORTS:
@@ -436,3 +458,216 @@ def decode_plan(head_recs, prompt_len, n_seqs, prompt_valid, static_valid, t_img
     n2 = int(load().ssd_debug_decode_plan(*args, out.ctypes.data, n))
     assert n2 == n
     return out[:n]
+
+
+_PAGED_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
+
+def _strides(t: torch.Tensor, n: int):
+    """The first n strides; 0 for dimensions of one element, whose stride says nothing."""
+    return [0 if t.shape[i] == 1 else t.stride(i) for i in range(n)]
+
+
+class PagedKV:
+    """A paged cache of one layer: a view of the caller's tensors plus a workspace.
+
+    k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim], bf16, fp16 or float8_e4m3fn, the last dimension
+                      contiguous, both with the same strides (pass ``pool.transpose(1, 2)`` for pages that hold a
+                      slot's heads side by side); [n_pages, 1, page_size, head_dim] where the table has a row per head
+    page_table        int32 [n_seqs, max_pages], or [n_seqs, n_kv_heads, max_pages]
+    lengths           int32 [n_seqs], or [n_seqs, n_kv_heads]: slots held
+    k_scales, v_scales  float32 [n_pages, n_kv_heads, page_size], 8-bit pages only
+    scores            float32 [n_seqs, n_kv_heads, slots]: weights each slot has had, for ``evict``
+
+    The tensors are read when the kernels run: lengths and tables may change between calls, and a captured call
+    follows them.  A handle (its workspace) is used on one stream at a time; handles used in turn on one stream may
+    share a workspace (``workspace=other.workspace`` after ``other.reserve``).
+    """
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *,
+                 k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None,
+                 scores: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 4 or k_pages.dtype not in _PAGED_DTYPES or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
+            raise ValueError("PagedKV: want k_pages and v_pages [n_pages, n_kv_heads, page_size, head_dim], bf16, fp16 or float8_e4m3fn")
+        n_pages, pool_heads, page_size, head_dim = k_pages.shape
+        if page_table.dim() not in (2, 3) or page_table.dtype != torch.int32 or (page_table.shape[-1] > 1 and page_table.stride(-1) != 1):
+            raise ValueError("PagedKV: want page_table int32 [n_seqs, max_pages] or [n_seqs, n_kv_heads, max_pages], rows contiguous")
+        n_seqs = page_table.shape[0]
+        heads = page_table.shape[1] if page_table.dim() == 3 else pool_heads
+        if pool_heads not in (1, heads):
+            raise ValueError(f"PagedKV: the table has rows for {heads} heads, the pages for {pool_heads}")
+        if lengths.dtype != torch.int32 or tuple(lengths.shape) not in ((n_seqs,), (n_seqs, heads)):
+            raise ValueError(f"PagedKV: want lengths int32 [{n_seqs}] or [{n_seqs}, {heads}]")
+        if min(k_pages.shape) < 1 or page_table.shape[-1] < 1:
+            raise ValueError("PagedKV: empty pages or an empty table")
+        if _strides(k_pages, 3) != _strides(v_pages, 3) or k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+            raise ValueError("PagedKV: k_pages and v_pages need the same strides, the last dimension contiguous")
+        e4m3 = k_pages.dtype == torch.float8_e4m3fn
+        if (k_scales is not None, v_scales is not None) != (e4m3, e4m3):
+            raise ValueError("PagedKV: row scales belong to float8_e4m3fn pages, and those need them")
+        if e4m3:
+            for s in (k_scales, v_scales):
+                if s.dtype != torch.float32 or s.shape != k_pages.shape[:3] or _strides(s, 3) != _strides(k_scales, 3):
+                    raise ValueError(f"PagedKV: want k_scales and v_scales float32 {tuple(k_pages.shape[:3])} with the same strides")
+        if scores is not None and (scores.dtype != torch.float32 or scores.dim() != 3 or tuple(scores.shape[:2]) != (n_seqs, heads)
+                                   or scores.shape[2] < 1 or (scores.shape[2] > 1 and scores.stride(2) != 1)):
+            raise ValueError(f"PagedKV: want scores float32 [{n_seqs}, {heads}, slots], rows contiguous")
+        tensors = [t for t in (k_pages, v_pages, page_table, lengths, k_scales, v_scales, scores, workspace) if t is not None]
+        if any(not t.is_cuda or t.device != k_pages.device for t in tensors):
+            raise ValueError("PagedKV: want CUDA tensors on one device; there is no CPU path")
+        self.k_pages, self.v_pages, self.page_table, self.lengths = k_pages, v_pages, page_table, lengths
+        self.k_scales, self.v_scales, self.scores = k_scales, v_scales, scores
+        self.n_seqs, self.n_kv_heads, self.head_dim, self.page_size = n_seqs, heads, head_dim, page_size
+        self.capacity = page_table.shape[-1] * page_size
+        self.device = k_pages.device
+        self.lib = load()
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        p, t, n = _strides(k_pages, 3), _strides(page_table, page_table.dim() - 1), _strides(lengths, lengths.dim())
+        s = _strides(k_scales, 3) if e4m3 else [0, 0, 0]
+        w = _strides(scores, 2) if scores is not None else [0, 0]
+        # one head in the pool: its pages belong to whichever head's table names them
+        self._kv = SsdPagedKv(ptr(k_pages), ptr(v_pages), ptr(k_scales), ptr(v_scales), ptr(page_table), ptr(lengths), ptr(scores),
+                              ptr(self._status), p[0], p[1], p[2], s[0], s[1], s[2], t[0], t[1] if len(t) > 1 else 0,
+                              n[0], n[1] if len(n) > 1 else 0, w[0], w[1], _PAGED_DTYPES[k_pages.dtype], n_seqs, heads, head_dim,
+                              page_size, n_pages, page_table.shape[-1], scores.shape[2] if scores is not None else 0)
+        self._attn = SsdPagedAttn(softmax_scale=float(softmax_scale))
+        self._scale = float(softmax_scale)
+        self.workspace = workspace
+        self._ready = set()                                  # (n_q_heads, accumulate) that the workspace is known to serve
+        torch.cuda.current_stream(self.device).synchronize() # the status word is zero before another stream's call
+
+    def _check(self, rc, what):
+        if rc != SSD_OK:
+            raise SsdError(rc, what)
+
+    def _call(self, fn, *args):
+        """fn(*args, stream) with the cache's device current."""
+        index = self.device.index
+        if torch.cuda.current_device() == index:
+            return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        with torch.cuda.device(index):
+            return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+
+    def reserve(self, n_q_heads: int, accumulate: bool = False):
+        """Makes the workspace large enough for attention of n_q_heads query heads (with their weights).  The first
+        call of a kind does it by itself, except while a CUDA graph is being captured."""
+        with torch.cuda.device(self.device):
+            need = int(self.lib.ssd_paged_workspace_bytes(C.byref(self._kv), int(n_q_heads), int(bool(accumulate))))
+            if need == 0:
+                raise SsdError(SSD_ERR_INVALID_ARG, "ssd_paged_workspace_bytes")
+            if self.workspace is None or self.workspace.numel() < need + 256:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("PagedKV: reserve() the workspace before capturing a graph")
+                self.workspace = torch.zeros(need + 256, dtype=torch.uint8, device=self.device)
+                torch.cuda.current_stream().synchronize()    # zero before any stream uses it
+                self._ready = set()
+        self._ready.add((n_q_heads, bool(accumulate)))
+
+    def _rows(self, t: torch.Tensor, heads: int, dtype, what: str):
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != dtype or t.device != self.device or t.stride(2) != 1:
+            raise ValueError(f"PagedKV: want {what} {dtype} [.., {heads}, {self.head_dim}] on {self.device}, rows contiguous; got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def _q_dtype(self, t: torch.Tensor, what: str):
+        pages = self.k_pages.dtype
+        if t.dtype != pages if pages != torch.float8_e4m3fn else t.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"PagedKV: {what} is {t.dtype}, the pages are {pages}")
+        return t.dtype
+
+    def append(self, k_new: torch.Tensor, v_new: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None):
+        """Stores the newest tokens, which ``lengths`` already count: k_new, v_new [n_seqs, n_kv_heads, head_dim], one
+        per sequence, or [n_tokens, ..] with cu_seqlens int32 [n_seqs + 1] (sequence b's are rows cu[b] .. cu[b+1]-1)."""
+        dtype = self._q_dtype(k_new, "k_new")
+        self._rows(k_new, self.n_kv_heads, dtype, "k_new")
+        self._rows(v_new, self.n_kv_heads, dtype, "v_new")
+        ks, vs = _strides(k_new, 2), _strides(v_new, 2)
+        if k_new.shape != v_new.shape or ks != vs:
+            raise ValueError("PagedKV: k_new and v_new need one shape and the same strides")
+        if cu_seqlens is None:
+            if k_new.shape[0] != self.n_seqs:
+                raise ValueError(f"PagedKV: {k_new.shape[0]} new rows for {self.n_seqs} sequences, without cu_seqlens")
+        elif cu_seqlens.dtype != torch.int32 or tuple(cu_seqlens.shape) != (self.n_seqs + 1,) or cu_seqlens.device != self.device or cu_seqlens.stride(0) != 1:
+            raise ValueError(f"PagedKV: want cu_seqlens int32 [{self.n_seqs + 1}] on {self.device}")
+        self._check(self._call(self.lib.ssd_paged_append, self._kv, k_new.data_ptr(), v_new.data_ptr(), _PAGED_DTYPES[dtype], ks[0], ks[1],
+                               None if cu_seqlens is None else cu_seqlens.data_ptr(), k_new.shape[0]), "ssd_paged_append")
+
+    def _attend(self, fn, what, q, k_new, v_new, out, return_lse, accumulate):
+        dtype = self._q_dtype(q, "q")
+        heads = q.shape[1] if q.dim() == 3 else -1
+        self._rows(q, heads, dtype, "q")
+        if q.shape[0] != self.n_seqs or heads < 1 or heads % self.n_kv_heads:
+            raise ValueError(f"PagedKV: q has {q.shape[0]} rows of {heads} heads, the cache {self.n_seqs} of {self.n_kv_heads}")
+        if accumulate and self.scores is None:
+            raise ValueError("PagedKV: accumulate needs a cache with scores")
+        if out is None:
+            out = torch.empty((self.n_seqs, heads, self.head_dim), dtype=dtype, device=self.device)
+        else:
+            self._rows(out, heads, dtype, "out")
+            if out.shape[0] != self.n_seqs:
+                raise ValueError(f"PagedKV: out has {out.shape[0]} rows, q {self.n_seqs}")
+        lse = torch.empty((self.n_seqs, heads), dtype=torch.float32, device=self.device) if return_lse else None
+        if (heads, bool(accumulate)) not in self._ready:
+            self.reserve(heads, accumulate)
+        a = self._attn
+        a.q, a.out, a.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        a.q_seq_stride, a.q_head_stride = _strides(q, 2)
+        a.out_seq_stride, a.out_head_stride = _strides(out, 2)
+        a.q_dtype, a.n_q_heads, a.accumulate = _PAGED_DTYPES[dtype], heads, int(bool(accumulate))
+        if k_new is not None:
+            self._rows(k_new, self.n_kv_heads, dtype, "k_new")
+            self._rows(v_new, self.n_kv_heads, dtype, "v_new")
+            ks, vs = _strides(k_new, 2), _strides(v_new, 2)
+            if k_new.shape[0] != self.n_seqs or k_new.shape != v_new.shape or ks != vs:
+                raise ValueError(f"PagedKV: want k_new and v_new [{self.n_seqs}, ..] with the same strides")
+            a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
+            a.new_seq_stride, a.new_head_stride = ks
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        a.workspace, a.workspace_bytes = base, self.workspace.numel() - (base - self.workspace.data_ptr())
+        self._check(self._call(fn, self._kv, a), what)
+        return (out, lse) if return_lse else out
+
+    def decode_attn(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, return_lse: bool = False, accumulate: bool = False):
+        """Attention of one new token per sequence, q [n_seqs, n_q_heads, head_dim], over all slots held (zeros where
+        there are none).  accumulate: adds every slot's weights, summed over the query heads, to ``scores``.
+        return_lse: also the log of the softmax's sum, float32 [n_seqs, n_q_heads], -inf where nothing is held."""
+        return self._attend(self.lib.ssd_paged_decode_attn, "ssd_paged_decode_attn", q, None, None, out, return_lse, accumulate)
+
+    def append_decode(self, k_new: torch.Tensor, v_new: torch.Tensor, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+                      return_lse: bool = False, accumulate: bool = False):
+        """append of one token per sequence, then decode_attn, in one launch."""
+        return self._attend(self.lib.ssd_paged_append_decode, "ssd_paged_append_decode", q, k_new, v_new, out, return_lse, accumulate)
+
+    def evict(self, prefix: int, budget, recent, into: Optional["PagedKV"] = None) -> torch.Tensor:
+        """Keeps, of every sequence and head with more than prefix + budget + recent slots, the first `prefix`, the
+        `budget` with the highest scores in between (ties: the lowest slot), and the last `recent`; budget and recent
+        are numbers or one number per head.  Moves them, in order, to the first slots of `into` (None: in place), with
+        their scores, and sets its lengths.  Returns the source slot of each kept token, int32 [n_seqs, n_kv_heads,
+        n], -1 behind the last one."""
+        if self.scores is None:
+            raise ValueError("PagedKV: evict needs a cache with scores")
+        h = self.n_kv_heads
+        b = [int(budget)] * h if np.ndim(budget) == 0 else [int(x) for x in budget]
+        r = [int(recent)] * h if np.ndim(recent) == 0 else [int(x) for x in recent]
+        if len(b) != h or len(r) != h or min(b) < 0 or min(r) < 0 or prefix < 0 or prefix + max(map(sum, zip(b, r))) >= 1 << 31:
+            raise ValueError(f"PagedKV: want prefix >= 0, and budget and recent >= 0, one or {h} of them")
+        if into is not None and into.device != self.device:
+            raise ValueError("PagedKV: both caches have to be on one device")
+        cols = max(1, min(int(prefix) + max(map(sum, zip(b, r))), self.capacity))
+        buf = torch.empty(self.n_seqs * h * (cols + 1), dtype=torch.int32, device=self.device)
+        kept = buf[: self.n_seqs * h * cols].view(self.n_seqs, h, cols)
+        ints = C.c_int32 * h
+        self._check(self._call(self.lib.ssd_paged_evict, self._kv, None if into is None else into._kv, int(prefix), ints(*b), ints(*r),
+                               buf.data_ptr(), cols, buf.data_ptr() + 4 * self.n_seqs * h * cols), "ssd_paged_evict")
+        return kept
+
+    def device_status(self) -> int:
+        """Bits of what the kernels met in tables, lengths and scores and left out (1 a page outside the pool, 2 a
+        length outside the table, 4 a slot behind its score row).  Synchronises."""
+        return int(self._status.item())
+
+
+def head_budgets(labels, window: int, sink_budget: int, sink_recent: int):
+    """(budget, recent) per head for ``PagedKV.evict`` from one layer's labels (Sec. 3.3): a semantic head keeps the
+    top-M and a short recent window, a spatial head its window."""
+    lab = np.asarray(labels).reshape(-1).astype(bool)
+    return np.where(lab, sink_budget, 0).tolist(), np.where(lab, sink_recent, window).tolist()

@@ -1,0 +1,639 @@
+// The paged cache: append, accumulation of the weights, eviction, and the host side of its C ABI.
+#include <cmath>
+
+#include "ssd_paged.cuh"
+
+namespace ssd {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ----------------------------------------------------------------------------- append
+// A warp takes four heads of one token (8 rows, K and V): 2 D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads
+// before the first store.  Bound by the bytes of the rows for a chunk of prompts, by latency for one decode step.
+constexpr int kAppendHeads = 4;
+
+struct AppendPagedParams {
+  PagedView c;
+  const char* k_new;
+  const char* v_new;
+  long long token_b, head_b;       // bytes
+  const int32_t* cu;               // or null: token i is the newest of sequence i
+  int n_tokens, bf16;
+};
+
+template <int D, bool kQ8>
+__global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid_constant__ AppendPagedParams p) {
+  constexpr int kL = D / 8, kRows = 32 / kL, kIters = 2 * kAppendHeads / kRows;
+  const PagedView& c = p.c;
+  const int lane = threadIdx.x & 31;
+  const int groups = (c.H + kAppendHeads - 1) / kAppendHeads;
+  const long long item = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const int token = (int)(item / groups), head0 = (int)(item % groups) * kAppendHeads;
+  if (token >= p.n_tokens) return;
+  int seq = token, ago = 1;
+  if (p.cu) {                                       // the last sequence that begins at or before the token
+    int a = 0, b = c.n_seqs;
+    while (a < b) {
+      const int m = (a + b) >> 1;
+      if (__ldg(p.cu + m) <= token) a = m + 1; else b = m;
+    }
+    seq = a - 1;
+    if (seq < 0) return;
+    ago = __ldg(p.cu + seq + 1) - token;            // 1 for a sequence's newest token
+    if (ago <= 0) return;
+  }
+  uint4 raw[kIters];
+#pragma unroll
+  for (int it = 0; it < kIters; ++it) {
+    const int r = it * kRows + lane / kL, head = head0 + (r >> 1);
+    raw[it] = make_uint4(0u, 0u, 0u, 0u);
+    if (head < c.H) raw[it] = __ldg(reinterpret_cast<const uint4*>((r & 1 ? p.v_new : p.k_new) + token * p.token_b + head * p.head_b) + lane % kL);
+  }
+#pragma unroll
+  for (int it = 0; it < kIters; ++it) {
+    const int r = it * kRows + lane / kL, head = head0 + (r >> 1), part = lane % kL;
+    bool ok = head < c.H;
+    int page = 0, row = 0;
+    if (ok) {
+      const int len = paged_length(c, seq, head);
+      const int slot = len - ago;
+      ok = slot >= 0;
+      if (!ok && (p.cu || len > 0)) paged_flag(c, kPagedBadLength);
+      if (ok) {
+        page = paged_lookup(c, paged_table(c, seq, head), slot, row);
+        ok = page >= 0;
+        if (ok && c.scores && part == 0 && !(r & 1)) {
+          if (slot < c.score_slots) paged_scores(c, seq, head)[slot] = 0.f;
+          else paged_flag(c, kPagedBadScores);
+        }
+      }
+    }
+    char* to = (r & 1 ? c.v : c.k) + page * c.page_b + head * c.head_b + row * c.slot_b;
+    if constexpr (kQ8) {
+      float scale;
+      const uint2 code = paged_quantize<kL>(raw[it], p.bf16 != 0, scale);
+      if (ok) {
+        reinterpret_cast<uint2*>(to)[part] = code;
+        if (part == 0) (r & 1 ? c.vs : c.ks)[page * c.sc_page + head * c.sc_head + row * c.sc_slot] = scale;
+      }
+    } else if (ok) {
+      reinterpret_cast<uint4*>(to)[part] = raw[it];
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- weights
+// scores += sum over the query heads of a key head of 2^(logit - m) / l, from the logits and (m, l) that the attention
+// launch before it left: 4 bytes read per query head and slot, against 2 row bytes of K and V there.
+constexpr int kWeightSlots = 4 * kThreads;          // slots of a thread block
+
+__global__ void __launch_bounds__(kThreads) ssd_paged_weights_kernel(const __grid_constant__ PagedDecodeParams p, int blocks_per_pair) {
+  __shared__ float2 s_ml[128];
+  const PagedView& c = p.c;
+  const int pair = blockIdx.x / blocks_per_pair, part = blockIdx.x - pair * blocks_per_pair;
+  const int seq = pair / c.H, head = pair - seq * c.H;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const int len = paged_length(c, seq, head);
+  const int first = part * kWeightSlots;
+  if (first >= len) return;
+  float* scores = paged_scores(c, seq, head);
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int h0 = 0; h0 < p.g; h0 += 128) {
+    const int n = min(128, p.g - h0);
+    __syncthreads();
+    for (int h = threadIdx.x; h < n; h += kThreads) {
+      float2 x = __ldg(p.ml + (size_t)pair * p.g + h0 + h);
+      x.y = x.y == 0.f ? 0.f : 1.f / x.y;
+      s_ml[h] = x;
+    }
+    __syncthreads();
+    const float* logits = p.logits + ((long long)pair * p.g + h0) * p.logit_row + first;
+#pragma unroll 4
+    for (int h = 0; h < n; ++h) {
+      const float2 ml = s_ml[h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = i * kThreads + threadIdx.x;
+        if (first + s < len) w[i] += ex2(__ldg(logits + h * p.logit_row + s) - ml.x) * ml.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int slot = first + i * kThreads + threadIdx.x;
+    if (slot >= len) continue;
+    if (slot >= c.score_slots) paged_flag(c, kPagedBadScores);
+    else if (p.k_new && slot == len - 1) scores[slot] = w[i];        // the token being appended has had none before
+    else scores[slot] += w[i];
+  }
+}
+
+// ----------------------------------------------------------------------------- eviction: which tokens stay
+struct EvictParams {
+  PagedView src, dst;
+  int in_place, dst_scores, prefix, kept_cols;
+  int32_t* kept;
+  int32_t* counts;
+  int keys_cap;                    // candidates whose keys fit in shared memory
+  int32_t budget[kMaxHeads], recent[kMaxHeads];
+};
+
+// Keys order as the scores do: unsigned integers, a NaN lowest, the two zeros equal.
+__device__ __forceinline__ uint32_t score_key(float x) {
+  if (x != x) return 0u;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// One thread block per (sequence, head): the budget-th largest key by digits of 11, 11 and 10 bits from the top (stopping
+// as soon as a digit's bin is taken whole), then the candidates above it and the first ones equal to it, in order.
+template <int kT>
+__global__ void __launch_bounds__(kT) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kBins = 2048, kW = kT / 32, kPer = kBins / kT;
+  extern __shared__ uint32_t s_keys[];
+  __shared__ uint32_t s_hist[kBins];
+  __shared__ uint32_t s_warp[kW], s_warp2[kW];
+  __shared__ uint32_t s_bin, s_need, s_whole;
+  const PagedView& c = p.src;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int pair = blockIdx.x, seq = pair / c.H, head = pair - seq * c.H;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const int n = paged_length(c, seq, head);
+  const int budget = p.budget[head], recent = p.recent[head], keep = p.prefix + budget + recent;
+  int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
+  const float* scores = paged_scores(c, seq, head);
+  const bool all = n <= keep;
+  const int count = all ? n : keep;
+
+  if (all) {
+    for (int j = tid; j < n; j += kT) kept[j] = j;
+  } else {
+    for (int j = tid; j < p.prefix; j += kT) kept[j] = j;
+    for (int j = tid; j < recent; j += kT) kept[p.prefix + budget + j] = n - recent + j;
+    const int nc = n - recent - p.prefix;                    // candidates: more than the budget
+    auto score_of = [&](int i) {
+      const int slot = p.prefix + i;
+      if (slot < c.score_slots) return scores[slot];
+      paged_flag(c, kPagedBadScores);
+      return 0.f;
+    };
+    const bool cached = nc <= p.keys_cap;
+    if (cached)
+      for (int i = tid; i < nc; i += kT) s_keys[i] = score_key(score_of(i));
+    auto key_of = [&](int i) { return cached ? s_keys[i] : score_key(score_of(i)); };
+    uint32_t prefix = 0u, mask = 0u, need = (uint32_t)budget;
+    bool whole = false;                                      // every key with this prefix is taken
+    for (int digit = 0; budget > 0 && digit < 3 && !whole; ++digit) {
+      const int shift = digit == 0 ? 21 : (digit == 1 ? 10 : 0);
+      const uint32_t width = digit == 2 ? 1023u : 2047u;
+      for (int b = tid; b < kBins; b += kT) s_hist[b] = 0u;
+      __syncthreads();
+      for (int i = tid; i < nc; i += kT) {
+        const uint32_t k = key_of(i);
+        if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & width], 1u);
+      }
+      __syncthreads();
+      // bins from the top: thread t has bins kBins - 1 - t * kPer and below
+      uint32_t own[kPer], sum = 0u;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        own[i] = s_hist[kBins - 1 - tid * kPer - i];
+        sum += own[i];
+      }
+      uint32_t inc = sum;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, inc, s);
+        if (lane >= s) inc += x;
+      }
+      if (lane == 31) s_warp[warp] = inc;
+      __syncthreads();
+      uint32_t before = inc - sum;
+      for (int w = 0; w < warp; ++w) before += s_warp[w];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (before < need && need <= before + own[i]) {
+          s_bin = kBins - 1 - tid * kPer - i;
+          s_need = need - before;
+          s_whole = need == before + own[i];
+        }
+        before += own[i];
+      }
+      __syncthreads();
+      prefix |= s_bin << shift;
+      mask |= width << shift;
+      need = s_need;
+      whole = s_whole != 0u;
+    }
+    // `need` of the candidates whose key has this prefix are taken (the first ones), and all above
+    if (budget > 0) {
+      __syncthreads();                                       // the keys, where no digit was looked at
+      const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
+      const int a = min(nc, warp * seg), b = min(nc, a + seg);
+      uint32_t above = 0u, equal = 0u;
+      for (int i0 = a; i0 < b; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t k = i < b ? key_of(i) & mask : 0u;
+        above += __popc(__ballot_sync(0xffffffffu, i < b && k > prefix));
+        equal += __popc(__ballot_sync(0xffffffffu, i < b && k == prefix));
+      }
+      if (lane == 0) { s_warp[warp] = above; s_warp2[warp] = equal; }
+      __syncthreads();
+      uint32_t g = 0u, e = 0u;
+      for (int w = 0; w < warp; ++w) { g += s_warp[w]; e += s_warp2[w]; }
+      const unsigned below = (1u << lane) - 1u;
+      for (int i0 = a; i0 < b; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t k = i < b ? key_of(i) & mask : 0u;
+        const unsigned mg = __ballot_sync(0xffffffffu, i < b && k > prefix);
+        const unsigned me = __ballot_sync(0xffffffffu, i < b && k == prefix);
+        const uint32_t gi = g + __popc(mg & below), ei = e + __popc(me & below);
+        if (i < b && (k > prefix || (k == prefix && ei < need))) kept[p.prefix + gi + min(ei, need)] = p.prefix + i;
+        g += __popc(mg);
+        e += __popc(me);
+      }
+    }
+  }
+  for (int j = count + tid; j < p.kept_cols; j += kT) kept[j] = -1;
+  if (tid == 0) p.counts[pair] = count;
+  if (!p.dst_scores || (all && p.in_place)) return;
+  // the scores travel with their tokens; in place, a slot's value is read before it is overwritten (sources lie at or
+  // above their destinations, so a round's writes touch nothing that a later round reads)
+  float* to = paged_scores(p.dst, seq, head);
+  __syncthreads();
+  for (int j0 = 0; j0 < count; j0 += kT) {
+    const int j = j0 + tid;
+    float x = 0.f;
+    if (j < count) {
+      const int s = kept[j];
+      if (s < c.score_slots) x = scores[s];
+    }
+    if (p.in_place) __syncthreads();
+    if (j < count) {
+      if (j < p.dst.score_slots) to[j] = x;
+      else paged_flag(p.dst, kPagedBadScores);
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- eviction: moving the rows
+// Row j of a head comes from slot kept[j] >= j.  Elsewhere: 2 row bytes / 16 lanes move a token (K and V), and a head's
+// tokens are shared out over gridDim.z thread blocks.  In place: the thread blocks of a head have 64 bytes of every
+// row each (blockIdx.y), so that the order that keeps it right (a round's rows are all read before the first is
+// written; later rounds read only above what it writes) is a matter of one thread block.
+template <int kRow, bool kInPlace>
+__global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kCpr = kRow / 16;                            // 16-byte chunks of a row; a token has twice as many
+  constexpr int kL = kInPlace ? 4 : 2 * kCpr;                // lanes of a token (of its part that this block moves)
+  constexpr int kRpi = 32 / kL, kU = 4;
+  constexpr int kRound = kThreads / 32 * kRpi * kU;          // tokens of a round
+  const PagedView& a = p.src;
+  const PagedView& b = p.dst;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int pair = blockIdx.x, seq = pair / a.H, head = pair - seq * a.H;
+  const int chunk = blockIdx.y * kL + lane % kL;
+  const bool is_v = chunk >= kCpr;
+  const int byte = (is_v ? chunk - kCpr : chunk) * 16;
+  const bool scales = a.ks != nullptr && (chunk == 0 || chunk == kCpr);
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const int count = __ldg(p.counts + pair);
+  const int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
+  if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) b.lens[seq * b.n_seq + head * b.n_head] = count;
+  const int32_t* ta = paged_table(a, seq, head);
+  const int32_t* tb = paged_table(b, seq, head);
+  const char* from = (is_v ? a.v : a.k) + head * a.head_b + byte;
+  char* to = (is_v ? b.v : b.k) + head * b.head_b + byte;
+  for (int j0 = blockIdx.z * kRound; j0 < count; j0 += gridDim.z * kRound) {
+    uint4 x[kU];
+    float sc[kU];
+    int page[kU], row[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = j0 + (u * (kThreads / 32) + warp) * kRpi + lane / kL;
+      page[u] = -1;
+      if (j < count) {
+        const int s = __ldg(kept + j);
+        if (!(kInPlace && s == j) && s >= 0 && s < a.cap) {
+          int r;
+          const int g = paged_lookup(a, ta, s, r);
+          page[u] = paged_lookup(b, tb, j, row[u]);
+          if (g < 0) page[u] = -1;
+          if (page[u] >= 0) {
+            x[u] = *reinterpret_cast<const uint4*>(from + g * a.page_b + r * a.slot_b);
+            if (scales) sc[u] = (is_v ? a.vs : a.ks)[g * a.sc_page + head * a.sc_head + r * a.sc_slot];
+          }
+        }
+      }
+    }
+    if constexpr (kInPlace) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (page[u] >= 0) {
+        *reinterpret_cast<uint4*>(to + page[u] * b.page_b + row[u] * b.slot_b) = x[u];
+        if (scales) (is_v ? b.vs : b.ks)[page[u] * b.sc_page + head * b.sc_head + row[u] * b.sc_slot] = sc[u];
+      }
+  }
+}
+
+// ----------------------------------------------------------------------------- host side
+template <class P>
+cudaError_t launch(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  count_launch();
+  return e;
+}
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int elem_bytes(int dtype) { return dtype == SSD_PAGED_E4M3 ? 1 : 2; }
+
+// A view of what the caller describes, or why not.
+int check_view(const ssd_paged_kv* k, PagedView* v) {
+  if (!k || !k->k_pages || !k->v_pages || !k->page_table || !k->lengths) return SSD_ERR_INVALID_ARG;
+  if (k->dtype < 0 || k->dtype > SSD_PAGED_E4M3 || (k->head_dim != 64 && k->head_dim != 128)) return SSD_ERR_INVALID_ARG;
+  if (k->n_seqs < 0 || k->n_kv_heads < 1 || k->page_size < 1 || k->n_pages < 1 || k->max_pages < 1) return SSD_ERR_INVALID_ARG;
+  if (k->dtype == SSD_PAGED_E4M3 ? !k->k_scales || !k->v_scales : k->k_scales || k->v_scales) return SSD_ERR_INVALID_ARG;
+  const int eb = elem_bytes(k->dtype);
+  const int64_t strides[] = {k->page_stride, k->head_stride, k->slot_stride};
+  for (int64_t s : strides)
+    if (s < 0 || s > (int64_t)1 << 48 || s * eb % 16 != 0) return SSD_ERR_INVALID_ARG;
+  const int64_t others[] = {k->scale_page_stride, k->scale_head_stride, k->scale_slot_stride, k->table_seq_stride, k->table_head_stride,
+                            k->len_seq_stride, k->len_head_stride, k->score_seq_stride, k->score_head_stride};
+  for (int64_t s : others)
+    if (s < 0 || s > (int64_t)1 << 48) return SSD_ERR_INVALID_ARG;
+  if (!aligned(k->k_pages, 16) || !aligned(k->v_pages, 16) || !aligned(k->k_scales, 4) || !aligned(k->v_scales, 4) ||
+      !aligned(k->page_table, 4) || !aligned(k->lengths, 4) || !aligned(k->scores, 4) || !aligned(k->status, 4))
+    return SSD_ERR_INVALID_ARG;
+  if (k->scores && k->score_slots < 1) return SSD_ERR_INVALID_ARG;
+  if (k->n_kv_heads > kMaxHeads || (int64_t)k->max_pages * k->page_size >= (int64_t)1 << 30) return SSD_ERR_LIMIT;
+  if ((int64_t)k->n_seqs * k->n_kv_heads > (int64_t)1 << 24) return SSD_ERR_LIMIT;
+  v->k = static_cast<char*>(k->k_pages);
+  v->v = static_cast<char*>(k->v_pages);
+  v->ks = k->k_scales;
+  v->vs = k->v_scales;
+  v->table = k->page_table;
+  v->lens = k->lengths;
+  v->scores = k->scores;
+  v->status = k->status;
+  v->page_b = k->page_stride * eb;
+  v->head_b = k->head_stride * eb;
+  v->slot_b = k->slot_stride * eb;
+  v->sc_page = k->scale_page_stride;
+  v->sc_head = k->scale_head_stride;
+  v->sc_slot = k->scale_slot_stride;
+  v->t_seq = k->table_seq_stride;
+  v->t_head = k->table_head_stride;
+  v->n_seq = k->len_seq_stride;
+  v->n_head = k->len_head_stride;
+  v->w_seq = k->score_seq_stride;
+  v->w_head = k->score_head_stride;
+  v->n_seqs = k->n_seqs;
+  v->H = k->n_kv_heads;
+  v->page_size = k->page_size;
+  v->page_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (k->page_size == 1 << s) v->page_shift = s;
+  v->n_pages = k->n_pages;
+  v->cap = k->max_pages * k->page_size;
+  v->score_slots = k->scores ? k->score_slots : 0;
+  return SSD_OK;
+}
+
+int sm_count(int* sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return SSD_ERR_CUDA;
+  }
+  return SSD_OK;
+}
+
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// [counters | partial states | (max, sum) | logits].  The counters, the only part that has to be zero between calls, lie
+// at the same place whatever the call's sizes: caches of any shapes can share a workspace.
+struct Workspace {
+  size_t partial, ml, logits, bytes;
+};
+
+Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate, int sms) {
+  const int rows = paged_rows(g);
+  const size_t heads = (size_t)v.n_seqs * v.H * g;
+  Workspace w;
+  w.partial = align_up(paged_max_workers(sms) * 4);
+  w.ml = align_up(w.partial + paged_max_workers(sms) * 2 * rows * (head_dim + 2) * 4);
+  w.logits = align_up(w.ml + (accumulate ? heads * 8 : 0));
+  w.bytes = w.logits + (accumulate ? heads * (size_t)v.cap * 4 : 0);
+  return w;
+}
+
+int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* stream) {
+  PagedDecodeParams p = {};
+  int rc = check_view(kv, &p.c);
+  if (rc != SSD_OK) return rc;
+  if (!a || !a->q || !a->out || !a->workspace || (append && (!a->k_new || !a->v_new))) return SSD_ERR_INVALID_ARG;
+  if (a->n_q_heads < 1 || a->n_q_heads % kv->n_kv_heads != 0) return SSD_ERR_INVALID_ARG;
+  if (a->q_dtype != SSD_PAGED_BF16 && a->q_dtype != SSD_PAGED_FP16) return SSD_ERR_INVALID_ARG;
+  if (kv->dtype != SSD_PAGED_E4M3 && a->q_dtype != kv->dtype) return SSD_ERR_INVALID_ARG;
+  if (!(a->softmax_scale >= 0.f) || !std::isfinite(a->softmax_scale)) return SSD_ERR_INVALID_ARG;
+  if (a->accumulate && !kv->scores) return SSD_ERR_INVALID_ARG;
+  const int64_t strides[] = {a->q_seq_stride, a->q_head_stride, a->out_seq_stride, a->out_head_stride,
+                             append ? a->new_seq_stride : 0, append ? a->new_head_stride : 0};
+  for (int64_t s : strides)
+    if (s < 0 || s > (int64_t)1 << 48 || s % 8 != 0) return SSD_ERR_INVALID_ARG;
+  if (!aligned(a->q, 16) || !aligned(a->out, 16) || (append && (!aligned(a->k_new, 16) || !aligned(a->v_new, 16))) || !aligned(a->lse, 4) ||
+      !aligned(a->workspace, 256))
+    return SSD_ERR_INVALID_ARG;
+  p.g = a->n_q_heads / kv->n_kv_heads;
+  p.rows = paged_rows(p.g);
+  p.qt = (p.g + p.rows - 1) / p.rows;
+  // tiles are counted in 32 bits (a tile has 16 slots at least)
+  if ((double)kv->n_seqs * kv->n_kv_heads * p.qt * (p.c.cap / 16 + 1) > 2.0e9) return SSD_ERR_LIMIT;
+  if (kv->n_seqs == 0) return SSD_OK;
+  int sms = 0;
+  rc = sm_count(&sms);
+  if (rc != SSD_OK) return rc;
+  const Workspace w = workspace_of(p.c, kv->head_dim, p.g, a->accumulate != 0, sms);
+  if (a->workspace_bytes < w.bytes) return SSD_ERR_NO_MEM;
+  p.q = static_cast<const char*>(a->q);
+  p.q_seq = a->q_seq_stride * 2;
+  p.q_head = a->q_head_stride * 2;
+  p.out = static_cast<char*>(a->out);
+  p.o_seq = a->out_seq_stride * 2;
+  p.o_head = a->out_head_stride * 2;
+  if (append) {
+    p.k_new = static_cast<const char*>(a->k_new);
+    p.v_new = static_cast<const char*>(a->v_new);
+    p.new_seq = a->new_seq_stride * 2;
+    p.new_head = a->new_head_stride * 2;
+  }
+  p.lse = a->lse;
+  char* ws = static_cast<char*>(a->workspace);
+  p.counters = reinterpret_cast<uint32_t*>(ws);
+  p.partial = reinterpret_cast<float*>(ws + w.partial);
+  if (a->accumulate) {
+    p.ml = reinterpret_cast<float2*>(ws + w.ml);
+    p.logits = reinterpret_cast<float*>(ws + w.logits);
+    p.logit_row = p.c.cap;
+  }
+  const float scale = a->softmax_scale > 0.f ? a->softmax_scale : 1.f / std::sqrt((float)kv->head_dim);
+  p.scale_log2 = scale * 1.44269504088896340736f;
+  p.bf16 = a->q_dtype == SSD_PAGED_BF16;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = kv->dtype == SSD_PAGED_E4M3 ? launch_paged_decode_8(p, kv->head_dim, sms, st) : launch_paged_decode_16(p, kv->head_dim, sms, st);
+  if (e == cudaSuccess && a->accumulate) e = launch_paged_weights(p, st);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_weights(const PagedDecodeParams& p, cudaStream_t st) {
+  const int per = (p.c.cap + kWeightSlots - 1) / kWeightSlots;
+  const long long blocks = (long long)p.c.n_seqs * p.c.H * per;
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, ssd_paged_weights_kernel, p, per);
+  count_launch();
+  return e;
+}
+
+}  // namespace ssd
+
+using namespace ssd;
+
+extern "C" size_t ssd_paged_workspace_bytes(const ssd_paged_kv* kv, int32_t n_q_heads, int32_t accumulate) {
+  PagedView v = {};
+  if (check_view(kv, &v) != SSD_OK || n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0) return 0;
+  int sms = 0;
+  if (sm_count(&sms) != SSD_OK) return 0;
+  return workspace_of(v, kv->head_dim, n_q_heads / kv->n_kv_heads, accumulate != 0, sms).bytes;
+}
+
+extern "C" int ssd_paged_append(const ssd_paged_kv* kv, const void* k_new, const void* v_new, int32_t new_dtype, int64_t new_token_stride,
+                                int64_t new_head_stride, const int32_t* cu_seqlens, int32_t n_tokens, void* stream) {
+  AppendPagedParams p = {};
+  const int rc = check_view(kv, &p.c);
+  if (rc != SSD_OK) return rc;
+  if (!k_new || !v_new || n_tokens < 0 || (!cu_seqlens && n_tokens != kv->n_seqs)) return SSD_ERR_INVALID_ARG;
+  if (new_dtype != SSD_PAGED_BF16 && new_dtype != SSD_PAGED_FP16) return SSD_ERR_INVALID_ARG;
+  if (kv->dtype != SSD_PAGED_E4M3 && new_dtype != kv->dtype) return SSD_ERR_INVALID_ARG;
+  if (new_token_stride < 0 || new_head_stride < 0 || new_token_stride > (int64_t)1 << 48 || new_head_stride > (int64_t)1 << 48 ||
+      new_token_stride % 8 != 0 || new_head_stride % 8 != 0 || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(cu_seqlens, 4))
+    return SSD_ERR_INVALID_ARG;
+  if (n_tokens == 0 || kv->n_seqs == 0) return SSD_OK;
+  p.k_new = static_cast<const char*>(k_new);
+  p.v_new = static_cast<const char*>(v_new);
+  p.token_b = new_token_stride * 2;
+  p.head_b = new_head_stride * 2;
+  p.cu = cu_seqlens;
+  p.n_tokens = n_tokens;
+  p.bf16 = new_dtype == SSD_PAGED_BF16;
+  const long long warps = (long long)n_tokens * ((kv->n_kv_heads + kAppendHeads - 1) / kAppendHeads);
+  const long long blocks = (warps * 32 + kThreads - 1) / kThreads;
+  if (blocks > 0x7fffffffll) return SSD_ERR_LIMIT;
+  const bool q8 = kv->dtype == SSD_PAGED_E4M3;
+  auto* kernel = kv->head_dim == 128 ? (q8 ? ssd_paged_append_kernel<128, true> : ssd_paged_append_kernel<128, false>)
+                                     : (q8 ? ssd_paged_append_kernel<64, true> : ssd_paged_append_kernel<64, false>);
+  const cudaError_t e = launch<AppendPagedParams>(kernel, dim3((unsigned)blocks), kThreads, 0, static_cast<cudaStream_t>(stream), p);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;
+}
+
+extern "C" int ssd_paged_decode_attn(const ssd_paged_kv* kv, const ssd_paged_attn* args, void* stream) { return attend(kv, args, false, stream); }
+
+extern "C" int ssd_paged_append_decode(const ssd_paged_kv* kv, const ssd_paged_attn* args, void* stream) { return attend(kv, args, true, stream); }
+
+extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into, int32_t prefix, const int32_t* budget_host, const int32_t* recent_host,
+                               int32_t* kept, int32_t kept_cols, int32_t* counts, void* stream) {
+  EvictParams p = {};
+  int rc = check_view(kv, &p.src);
+  if (rc != SSD_OK) return rc;
+  if (!kv->scores || !budget_host || !recent_host || !kept || !counts || prefix < 0 || kept_cols < 1) return SSD_ERR_INVALID_ARG;
+  if (!aligned(kept, 4) || !aligned(counts, 4)) return SSD_ERR_INVALID_ARG;
+  if (into) {
+    rc = check_view(into, &p.dst);
+    if (rc != SSD_OK) return rc;
+    if (into->dtype != kv->dtype || into->head_dim != kv->head_dim || into->n_kv_heads != kv->n_kv_heads || into->n_seqs != kv->n_seqs)
+      return SSD_ERR_INVALID_ARG;
+    if (into == kv || into->page_table == kv->page_table || into->lengths == kv->lengths || (into->scores && into->scores == kv->scores))
+      return SSD_ERR_INVALID_ARG;                            // in place is into == NULL
+  } else {
+    p.dst = p.src;
+  }
+  int64_t most = 0;
+  bool same = true;
+  for (int h = 0; h < kv->n_kv_heads; ++h) {
+    if (budget_host[h] < 0 || recent_host[h] < 0) return SSD_ERR_INVALID_ARG;
+    const int64_t keep = (int64_t)prefix + budget_host[h] + recent_host[h];
+    if (keep > 0x7fffffffll) return SSD_ERR_LIMIT;
+    most = keep > most ? keep : most;
+    same &= budget_host[h] + recent_host[h] == budget_host[0] + recent_host[0];
+    p.budget[h] = budget_host[h];
+    p.recent[h] = recent_host[h];
+  }
+  if (p.dst.n_head == 0 && kv->n_kv_heads > 1 && !(same && p.src.n_head == 0)) return SSD_ERR_INVALID_ARG;
+  if (most > p.src.cap) most = p.src.cap;
+  if (kept_cols < most || p.dst.cap < most) return SSD_ERR_INVALID_ARG;
+  if (kv->n_seqs == 0) return SSD_OK;
+  p.in_place = into == nullptr;
+  p.dst_scores = p.dst.scores != nullptr;
+  p.prefix = prefix;
+  p.kept = kept;
+  p.kept_cols = kept_cols;
+  p.counts = counts;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int pairs = kv->n_seqs * kv->n_kv_heads;
+  // Short rows: 256 threads, so that several heads share an SM.  Long ones: 1024, and up to 48 K keys in shared memory.
+  cudaError_t e;
+  if (p.src.cap <= 8192) {
+    p.keys_cap = p.src.cap;
+    e = launch<EvictParams>(ssd_paged_select_kernel<256>, dim3(pairs), 256, (size_t)p.keys_cap * 4, st, p);
+  } else {
+    p.keys_cap = p.src.cap < 49152 ? p.src.cap : 49152;
+    e = cudaFuncSetAttribute(ssd_paged_select_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, 49152 * 4);
+    if (e == cudaSuccess) e = launch<EvictParams>(ssd_paged_select_kernel<1024>, dim3(pairs), 1024, (size_t)p.keys_cap * 4, st, p);
+  }
+  if (e == cudaSuccess) {
+    const int row = kv->head_dim * elem_bytes(kv->dtype);
+    // elsewhere: enough thread blocks for the whole GPU, each with one round of tokens at least
+    int z = 1;
+    if (into) {
+      const int round = kThreads * 4 / (2 * row / 16);
+      const int rounds = (int)((most + round - 1) / round);
+      z = (int)((148 * 8 + pairs - 1) / pairs);
+      z = z < 1 ? 1 : (z > rounds ? (rounds < 1 ? 1 : rounds) : z);
+    }
+    const dim3 grid(pairs, into ? 1 : 2 * row / 64, z);
+    auto* kernel = row == 256 ? (into ? ssd_paged_move_kernel<256, false> : ssd_paged_move_kernel<256, true>)
+                              : (row == 128 ? (into ? ssd_paged_move_kernel<128, false> : ssd_paged_move_kernel<128, true>)
+                                            : (into ? ssd_paged_move_kernel<64, false> : ssd_paged_move_kernel<64, true>));
+    e = launch<EvictParams>(kernel, grid, kThreads, 0, st, p);
+  }
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;
+}

@@ -1,0 +1,926 @@
+// Attention of one new token over the paged cache (and, fused, the append of that token's rows): one launch.
+//
+// For a key head with n slots and the g query heads that share it:
+//   x_hj = scale q_h . k_j,   m_h = max_j x_hj,   l_h = sum_j e^(x_hj - m_h),   o_h = sum_j e^(x_hj - m_h) v_j / l_h.
+// One pass over K and V with a running maximum and sum; every byte of them is read once per group of <= 16 query heads.
+//
+// Work: the slots of a key head are cut into tiles of 8 KB (4 KB of K, 4 KB of V).  The tiles of all (sequence, head,
+// group) are one stream, cut into equal shares, one per worker, from the lengths that the launch finds on the device.
+// A worker is one warp (kWpw = 1), or the 8 warps of a thread block (kWpw = 8), which take a head's tiles in turn and
+// merge their states in shared memory.  Heads cut by a share's border leave (O, m, l) of each piece in global memory;
+// whoever completes the last piece (a counter, kept under the worker that has the head's first piece: a worker has at
+// most one head that starts in its share and is cut at its end) merges them in the order of the workers: the result does not
+// depend on who that is, and nobody waits for another.
+//
+// A warp keeps kStages tiles of its own in shared memory and fills them with 16-byte asynchronous copies, row by row
+// (pages may have any size and strides), zeros in the place of rows that do not exist: a NaN behind the last row, or
+// in a page that the table does not name, is never read.  No barrier between warps while tiles stream.
+//
+// Products on the tensor cores, transposed: S^T = K Q^T and O^T = V^T P^T, so that the keys and the head dimension
+// fill the 16 rows of an m16n8k16 product and the query heads its 8 columns (kNt = 2: 16 heads).  The work is bound by
+// the bytes of K and V (per 8 KB tile: 24 products and 16 ldmatrix for 8 heads, a fraction of the 8 KB's time on HBM).
+// The weights are rounded to 16 bits for the second product as a sum of two 16-bit terms, which keeps 16 (bf16) or 22
+// (fp16) bits of them; all sums are in 32 bits.  The weights are held 2^14 times too large (kShift) so that the small
+// ones of a long row stay normal numbers in fp16; the factor is in l too and cancels.
+// 8-bit rows are widened to fp16, which holds every code exactly; q is brought into fp16's range by a power of two per
+// head, the K scale multiplies the logit, and the V scale's power of two 2^e is added to it: the running maximum is that
+// of x + e, so that a weight times its V scale is 2^15 at most whatever the scales of other rows; l takes 2^-e back out.
+#pragma once
+
+#include <atomic>
+
+#include "ssd_paged.cuh"
+
+namespace ssd {
+namespace paged {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr float kShift = 14.f;
+constexpr float kNegInf = -__builtin_huge_valf();
+
+template <int D, int kFmt>
+struct Geo {
+  static constexpr int kRow = kFmt == kPagedE4m3 ? D : 2 * D;      // bytes of a row in a page
+  static constexpr int kTile = 4096 / kRow;                        // keys of a tile
+  static constexpr int kCpr = kRow / 16;                           // 16-byte chunks of a row
+  static constexpr int kRpl = (kTile + 31) / 32;                   // rows of a tile whose address a lane works out
+  static constexpr int kScaleBytes = kFmt == kPagedE4m3 ? kTile * 8 : 0;
+  static constexpr int kMaskAt = 8192 + kScaleBytes;               // 2 words: which rows exist
+  static constexpr int kStage = (kMaskAt + 8 + 127) / 128 * 128;
+  static constexpr int kStages = 3;
+  static constexpr int kRing = kStage * kStages;
+  static constexpr int kSmem = kRing * kWarps;
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  if constexpr (kBf16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+// (a, b) as a sum of two pairs of 16-bit numbers, a in the low half
+template <bool kBf16>
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  if constexpr (kBf16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    const float2 f = __bfloat1622float2(h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(a - f.x, b - f.y);
+    memcpy(&hi, &h, 4);
+    memcpy(&lo, &l, 4);
+  } else {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+    memcpy(&hi, &h, 4);
+    memcpy(&lo, &l, 4);
+  }
+}
+// two E4M3 codes (low and high half word of c hold two each) -> two fp16, exactly
+__device__ __forceinline__ uint32_t widen_lo(uint32_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)(c & 0xffffu)));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)(c >> 16)));
+  return r;
+}
+__device__ __forceinline__ void store16(char* to, float x, bool bf16) {
+  if (bf16)
+    *reinterpret_cast<__nv_bfloat16*>(to) = __float2bfloat16_rn(x);
+  else
+    *reinterpret_cast<__half*>(to) = __float2half_rn(x);
+}
+
+// A place in the stream of tiles.
+struct Place {
+  int vp;        // (sequence * H + head) * qt + group
+  int t, end;    // tile of the head, and the tile behind the worker's last one of this head
+  int len;
+};
+
+template <int D, int kFmt, int kNt>
+struct Worker {
+  using G = Geo<D, kFmt>;
+  static constexpr bool kBf16 = kFmt == kPagedBf16;        // type of the products' operands
+  static constexpr int kKs = D / 16;
+  const PagedDecodeParams& p;
+  const int lane;
+  const uint32_t ring;      // shared memory of this warp
+  unsigned char* ring_ptr;
+  // the state of the head being summed
+  uint32_t qf[kNt][kKs][2];
+  float cs[kNt][2];         // scale of the logits (base 2) of this thread's two columns
+  float o[kNt][kKs][4];
+  float m[kNt][2], l[kNt][2];
+
+  __device__ Worker(const PagedDecodeParams& p_, int lane_, unsigned char* mem)
+      : p(p_), lane(lane_), ring(smem_u32(mem)), ring_ptr(mem) {}
+
+  // dimension of the O accumulator c[0], c[1] (half 0) or c[2], c[3] (half 1) of product mt
+  __device__ __forceinline__ int dim_of(int mt, int half) const {
+    return kFmt == kPagedE4m3 ? 16 * mt + 2 * (lane >> 2) + half : 16 * mt + 8 * half + (lane >> 2);
+  }
+
+  __device__ __forceinline__ void begin(int seq, int head, int qi) {
+    const int n_q = min(p.g - qi * p.rows, p.rows);
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt) {
+      const int h = nt * 8 + (lane >> 2);
+      const char* q = p.q + seq * p.q_seq + ((long long)head * p.g + qi * p.rows + h) * p.q_head;
+      const int at = kFmt == kPagedE4m3 ? 8 * (lane & 3) : 4 * (lane & 3);   // bytes; which dimensions is the K side's order
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks) {
+        uint2 w = make_uint2(0u, 0u);
+        if (h < n_q) {
+          if constexpr (kFmt == kPagedE4m3) {
+            w = *reinterpret_cast<const uint2*>(q + 32 * ks + at);
+          } else {
+            w.x = *reinterpret_cast<const uint32_t*>(q + 32 * ks + at);
+            w.y = *reinterpret_cast<const uint32_t*>(q + 32 * ks + 16 + at);
+          }
+        }
+        qf[nt][ks][0] = w.x;
+        qf[nt][ks][1] = w.y;
+      }
+      float by = 1.f;
+      if constexpr (kFmt == kPagedE4m3) {
+        // fp16 copies of q: a power of two brings the head's largest value to [2^11, 2^12), which loses nothing that
+        // 24 bits of the products' sum would show (what falls below fp16's smallest step is 2^-36 of the largest)
+        float x[kKs][4], top = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float2 f;
+            if (p.bf16) {
+              f = widen2(qf[nt][ks][i]);
+            } else {
+              __half2 hh;
+              memcpy(&hh, &qf[nt][ks][i], 4);
+              f = __half22float2(hh);
+            }
+            x[ks][2 * i] = f.x;
+            x[ks][2 * i + 1] = f.y;
+            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^(11 - floor(log2 top)), its exponent kept where the inverse is a normal number too
+        int e = 127 + 11 - (int)(__float_as_uint(top) >> 23);
+        e = top > 0.f ? max(-112, min(e, 112)) : 0;
+        const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+        by = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const __half2 hh = __floats2half2_rn(x[ks][2 * i] * up, x[ks][2 * i + 1] * up);
+            memcpy(&qf[nt][ks][i], &hh, 4);
+          }
+      }
+      // the logits' columns of this thread are heads 2 (lane & 3) and the next one
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        cs[nt][e] = p.scale_log2 * (kFmt == kPagedE4m3 ? __shfl_sync(0xffffffffu, by, ((2 * (lane & 3) + e) * 4)) : 1.f);
+#pragma unroll
+      for (int mt = 0; mt < kKs; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
+      m[nt][0] = m[nt][1] = kNegBig;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+  }
+
+  // ---------------------------------------------------------------- loading
+  // Looks up the rows of a tile (this lane's ones) in the table; the loads' latency passes during the tile before.
+  struct Rows {
+    int page[G::kRpl], row[G::kRpl];
+  };
+  __device__ __forceinline__ void look_up(const Place& at, int seq, int head, Rows& r) const {
+    const int32_t* table = paged_table(p.c, seq, head);
+#pragma unroll
+    for (int i = 0; i < G::kRpl; ++i) {
+      const int local = i * 32 + lane;
+      const int slot = at.t * G::kTile + local;
+      r.page[i] = -1;
+      r.row[i] = 0;
+      if (local < G::kTile && slot < at.len) {
+        int index;
+        paged_split(p.c, slot, index, r.row[i]);
+        r.page[i] = __ldg(table + index);
+      }
+    }
+  }
+
+  __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) const {
+    // eight rows of one chunk number lie in eight different 16-byte columns of the banks: ldmatrix without conflicts
+    if constexpr (G::kCpr >= 8) return row * G::kRow + ((chunk ^ (row & 7)) << 4);
+    return row * G::kRow + ((chunk ^ ((row >> 1) & 3)) << 4);
+  }
+
+  __device__ __forceinline__ void issue(const Place& at, int seq, int head, int qi, int stage, const Rows& r) {
+    const uint32_t base = ring + stage * G::kStage;
+    const PagedView& c = p.c;
+    const bool fused = p.k_new != nullptr;
+    const int last = at.len - 1 - at.t * G::kTile;           // the new row's place in this tile, if it is in it
+    long long off[G::kRpl];
+    uint32_t have[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < G::kRpl; ++i) {
+      const int local = i * 32 + lane;
+      const bool held = local < G::kTile && at.t * G::kTile + local < at.len;
+      const bool ok = held && (uint32_t)r.page[i] < (uint32_t)c.n_pages;
+      if (held && !ok) paged_flag(c, kPagedBadPage);
+      off[i] = ok && !(fused && local == last) ? r.page[i] * c.page_b + head * c.head_b + r.row[i] * c.slot_b : -1;
+      have[i] = __ballot_sync(0xffffffffu, ok);
+      if constexpr (kFmt == kPagedE4m3) {
+        const long long so = ok ? r.page[i] * c.sc_page + head * c.sc_head + r.row[i] * c.sc_slot : 0;
+        if (local < G::kTile && !(fused && local == last)) {
+          cp4(base + 8192 + local * 4, c.ks + so, ok);
+          cp4(base + 8192 + G::kTile * 4 + local * 4, c.vs + so, ok);
+        }
+      }
+    }
+    constexpr int kRpi = 32 / G::kCpr;                       // rows that one copy instruction of the warp brings
+    const int chunk = lane % G::kCpr;
+#pragma unroll
+    for (int it = 0; it < G::kTile / kRpi; ++it) {
+      const int row = it * kRpi + lane / G::kCpr;
+      const long long f = __shfl_sync(0xffffffffu, off[(it * kRpi) / 32], row & 31);
+      const uint32_t to = base + chunk_at(row, chunk);
+      const long long from = (f < 0 ? 0 : f) + chunk * 16;
+      if (!(fused && row == last)) {
+        cp16(to, c.k + from, f >= 0);
+        cp16(to + 4096, c.v + from, f >= 0);
+      }
+    }
+    if (fused && last >= 0 && last < G::kTile) put_new(at, seq, head, qi, base, last, r);
+    if (lane == 0) {
+      uint32_t* mask = reinterpret_cast<uint32_t*>(ring_ptr + stage * G::kStage + G::kMaskAt);
+      mask[0] = have[0];
+      mask[1] = have[1];
+    }
+  }
+
+  // The rows of the token being appended: from k_new and v_new into the stage and, by the first group's worker, into
+  // their page.  Nothing else of this launch reads that slot.
+  __device__ __noinline__ void put_new(const Place& at, int seq, int head, int qi, uint32_t base, int last, const Rows& r) {
+    const PagedView& c = p.c;
+    constexpr int kL = D / 8;                                // lanes that hold a row, 8 values each; V from lane 16 on
+    const int part = lane & 15;
+    const bool mine = part < kL;
+    const char* from = (lane < 16 ? p.k_new : p.v_new) + seq * p.new_seq + head * p.new_head;
+    const uint4 raw = mine ? __ldg(reinterpret_cast<const uint4*>(from) + part) : make_uint4(0u, 0u, 0u, 0u);
+    const int page = __shfl_sync(0xffffffffu, r.page[last / 32], last & 31);
+    const int row = __shfl_sync(0xffffffffu, r.row[last / 32], last & 31);
+    const bool ok = (uint32_t)page < (uint32_t)c.n_pages;
+    const bool store = ok && qi == 0;
+    const long long off = ok ? page * c.page_b + head * c.head_b + row * c.slot_b : 0;
+    char* to = (lane < 16 ? c.k : c.v) + off;
+    const uint32_t sm = base + (lane < 16 ? 0u : 4096u);
+    if constexpr (kFmt == kPagedE4m3) {
+      float scale;
+      const uint2 code = paged_quantize<kL>(raw, p.bf16 != 0, scale);
+      if (mine) {
+        asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(sm + chunk_at(last, part >> 1) + (part & 1) * 8),
+                     "r"(ok ? code.x : 0u), "r"(ok ? code.y : 0u) : "memory");
+        if (store) reinterpret_cast<uint2*>(to)[part] = code;
+      }
+      if (part == 0) {
+        const uint32_t sc = base + 8192 + (lane < 16 ? 0 : G::kTile * 4) + last * 4;
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc), "r"(ok ? __float_as_uint(scale) : 0u) : "memory");
+        if (store) (lane < 16 ? c.ks : c.vs)[page * c.sc_page + head * c.sc_head + row * c.sc_slot] = scale;
+      }
+    } else if (mine) {
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(sm + chunk_at(last, part)), "r"(ok ? raw.x : 0u),
+                   "r"(ok ? raw.y : 0u), "r"(ok ? raw.z : 0u), "r"(ok ? raw.w : 0u) : "memory");
+      if (store) reinterpret_cast<uint4*>(to)[part] = raw;
+    }
+    // the new token has had no weight yet (where this step's weights are wanted, their kernel starts it)
+    if (store && c.scores && !p.logits && lane == 0 && at.len <= c.score_slots) paged_scores(c, seq, head)[at.len - 1] = 0.f;
+  }
+
+  // ---------------------------------------------------------------- one tile
+  __device__ __forceinline__ void consume(const Place& at, int seq, int head, int qi, int stage) {
+    constexpr int kSub = G::kTile / 16;
+    const uint32_t base = ring + stage * G::kStage;
+    const unsigned char* mem = ring_ptr + stage * G::kStage;
+    float s[kSub][kNt][4];
+    float vinv[kSub][2], vman[kSub][2];                      // 2^-e, and the V scale times that
+    const int j8 = lane >> 2, mi = lane >> 3, ml8 = lane & 7;
+#pragma unroll
+    for (int sb = 0; sb < kSub; ++sb) {
+#pragma unroll
+      for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[sb][nt][i] = 0.f;
+      const int krow = sb * 16 + (mi & 1) * 8 + ml8;         // keys of matrix mi: halves alternate, then chunks
+      if constexpr (kFmt == kPagedE4m3) {
+#pragma unroll
+        for (int c2 = 0; c2 < kKs / 2; ++c2) {
+          uint32_t r[4];
+          ldsm4(r, base + chunk_at(krow, 2 * c2 + (mi >> 1)));
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t a[4] = {widen_lo(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u]), widen_hi(r[2 * u + 1])};
+#pragma unroll
+            for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(s[sb][nt], a, qf[nt][2 * c2 + u]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+          uint32_t a[4];
+          ldsm4(a, base + chunk_at(krow, 2 * ks + (mi >> 1)));
+#pragma unroll
+          for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(s[sb][nt], a, qf[nt][ks]);
+        }
+      }
+    }
+    // logits in base 2, rows that do not exist at -inf
+    const uint32_t* have = reinterpret_cast<const uint32_t*>(mem + G::kMaskAt);
+#pragma unroll
+    for (int sb = 0; sb < kSub; ++sb) {
+      const uint32_t word = have[sb >> 1] >> ((sb & 1) * 16 + j8);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {                       // key j8 + 8 hf of the 16
+        const bool ok = (word >> (8 * hf)) & 1u;
+        const float kscale = kFmt == kPagedE4m3 ? reinterpret_cast<const float*>(mem + 8192)[sb * 16 + j8 + 8 * hf] : 1.f;
+#pragma unroll
+        for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float& x = s[sb][nt][2 * hf + e];
+            x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kNegInf;
+          }
+      }
+    }
+    if (p.logits) {
+      const int n_q = min(p.g - qi * p.rows, p.rows);
+      float* to = p.logits + (((long long)seq * p.c.H + head) * p.g + qi * p.rows) * p.logit_row + at.t * G::kTile;
+#pragma unroll
+      for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int h = nt * 8 + 2 * (lane & 3) + e;
+          if (h < n_q) {
+#pragma unroll
+            for (int sb = 0; sb < kSub; ++sb)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                const int key = sb * 16 + j8 + 8 * hf;
+                if (at.t * G::kTile + key < at.len) to[h * p.logit_row + key] = s[sb][nt][2 * hf + e];
+              }
+          }
+        }
+    }
+    float top[kNt][2];
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt) top[nt][0] = top[nt][1] = kNegInf;
+#pragma unroll
+    for (int sb = 0; sb < kSub; ++sb)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        float add = 0.f;
+        if constexpr (kFmt == kPagedE4m3) {
+          // e between bounds that keep l (sums of 2^(14 - e)) and the weights in float32's range; below 2^-100 the scale
+          // itself says how small the row is
+          const float vs = reinterpret_cast<const float*>(mem + 8192)[G::kTile + sb * 16 + j8 + 8 * hf];
+          const int e = max(-100, min((int)(__float_as_uint(vs) >> 23) - 127, 126));
+          vinv[sb][hf] = __uint_as_float((uint32_t)(127 - e) << 23);
+          vman[sb][hf] = vs * vinv[sb][hf];
+          add = (float)e;
+        }
+#pragma unroll
+        for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float& x = s[sb][nt][2 * hf + e];
+            if constexpr (kFmt == kPagedE4m3) x += add;
+            top[nt][e] = fmaxf(top[nt][e], x);
+          }
+      }
+    bool grown = false;
+    float fix[kNt][2];
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float t = top[nt][e];
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+        const float mn = fmaxf(m[nt][e], t);
+        fix[nt][e] = ex2(m[nt][e] - mn);
+        grown |= mn != m[nt][e];
+        m[nt][e] = mn;
+        l[nt][e] *= fix[nt][e];
+      }
+    if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+      for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < kKs; ++mt) {
+          o[nt][mt][0] *= fix[nt][0];
+          o[nt][mt][1] *= fix[nt][1];
+          o[nt][mt][2] *= fix[nt][0];
+          o[nt][mt][3] *= fix[nt][1];
+        }
+    }
+#pragma unroll
+    for (int sb = 0; sb < kSub; ++sb) {
+      uint32_t bh[kNt][2], bl[kNt][2];
+#pragma unroll
+      for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          float w0 = ex2(s[sb][nt][2 * hf] - (m[nt][0] - kShift));
+          float w1 = ex2(s[sb][nt][2 * hf + 1] - (m[nt][1] - kShift));
+          if constexpr (kFmt == kPagedE4m3) {
+            l[nt][0] = fmaf(w0, vinv[sb][hf], l[nt][0]);
+            l[nt][1] = fmaf(w1, vinv[sb][hf], l[nt][1]);
+            w0 *= vman[sb][hf];
+            w1 *= vman[sb][hf];
+          } else {
+            l[nt][0] += w0;
+            l[nt][1] += w1;
+          }
+          uint32_t hi, lo;
+          split2<kBf16>(w0, w1, hi, lo);
+          bh[nt][hf] = transpose8(hi);
+          bl[nt][hf] = transpose8(lo);
+        }
+      if constexpr (kFmt == kPagedE4m3) {
+        const int vrow = sb * 16 + (mi & 1) * 8 + ml8;
+#pragma unroll
+        for (int c2 = 0; c2 < kKs / 2; ++c2) {
+          uint32_t r[4];
+          ldsm4t(r, base + 4096 + chunk_at(vrow, 2 * c2 + (mi >> 1)));
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t x = __byte_perm(r[2 * u], 0u, 0x3120), y = __byte_perm(r[2 * u + 1], 0u, 0x3120);
+            const uint32_t a[4] = {widen_lo(x), widen_hi(x), widen_lo(y), widen_hi(y)};
+#pragma unroll
+            for (int nt = 0; nt < kNt; ++nt) {
+              mma<kBf16>(o[nt][2 * c2 + u], a, bh[nt]);
+              mma<kBf16>(o[nt][2 * c2 + u], a, bl[nt]);
+            }
+          }
+        }
+      } else {
+        const int vrow = sb * 16 + (mi >> 1) * 8 + ml8;
+#pragma unroll
+        for (int mt = 0; mt < kKs; ++mt) {
+          uint32_t a[4];
+          ldsm4t(a, base + 4096 + chunk_at(vrow, 2 * mt + (mi & 1)));
+#pragma unroll
+          for (int nt = 0; nt < kNt; ++nt) {
+            mma<kBf16>(o[nt][mt], a, bh[nt]);
+            mma<kBf16>(o[nt][mt], a, bl[nt]);
+          }
+        }
+      }
+    }
+  }
+
+  // Sums of the lanes that share a column; every lane ends with its columns' (m, l).
+  __device__ __forceinline__ void close() {
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float t = l[nt][e];
+        t += __shfl_xor_sync(0xffffffffu, t, 4);
+        t += __shfl_xor_sync(0xffffffffu, t, 8);
+        t += __shfl_xor_sync(0xffffffffu, t, 16);
+        l[nt][e] = t;
+      }
+  }
+
+  __device__ __forceinline__ void write_state(float* to, int n_q) const {    // [rows][D], then m[rows], l[rows]
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int h = nt * 8 + 2 * (lane & 3) + e;
+        if (h < n_q) {
+#pragma unroll
+          for (int mt = 0; mt < kKs; ++mt) {
+            to[h * D + dim_of(mt, 0)] = o[nt][mt][e];
+            to[h * D + dim_of(mt, 1)] = o[nt][mt][2 + e];
+          }
+          if ((lane >> 2) == 0) {
+            to[p.rows * D + h] = m[nt][e];
+            to[p.rows * D + p.rows + h] = l[nt][e];
+          }
+        }
+      }
+  }
+
+  __device__ __forceinline__ void write_out(int seq, int head, int qi) const {
+    const int n_q = min(p.g - qi * p.rows, p.rows);
+#pragma unroll
+    for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int h = nt * 8 + 2 * (lane & 3) + e;
+        if (h < n_q) {
+          const long long qh = (long long)head * p.g + qi * p.rows + h;
+          char* to = p.out + seq * p.o_seq + qh * p.o_head;
+          const float by = l[nt][e] > 0.f ? 1.f / l[nt][e] : l[nt][e];       // no row at all: zeros (a NaN stays one)
+#pragma unroll
+          for (int mt = 0; mt < kKs; ++mt) {
+            store16(to + 2 * dim_of(mt, 0), o[nt][mt][e] * by, p.bf16 != 0);
+            store16(to + 2 * dim_of(mt, 1), o[nt][mt][2 + e] * by, p.bf16 != 0);
+          }
+          if ((lane >> 2) == 0) write_stats(p, seq, qh, m[nt][e], l[nt][e]);
+        }
+      }
+  }
+
+  static __device__ __forceinline__ void write_stats(const PagedDecodeParams& p, int seq, long long qh, float m, float l) {
+    const long long at = (long long)seq * p.c.H * p.g + qh;
+    if (p.lse) p.lse[at] = l == 0.f ? kNegInf : (m + log2f(l) - kShift) * 0.69314718055994530942f;
+    if (p.ml) p.ml[at] = make_float2(m - kShift, l);
+  }
+};
+
+// Merge of n pieces of one query head, by a warp: piece(i) gives the state's memory (global: read past L1).
+template <int D, class F>
+__device__ __forceinline__ void merge_head(const PagedDecodeParams& p, int lane, int h, int n, F piece, float (&o)[D / 32], float& m, float& l) {
+  m = kNegBig;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, __ldcg(piece(i) + p.rows * D + h));
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+  l = 0.f;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) o[d] = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const float* s = piece(i);
+    const float f = ex2(__ldcg(s + p.rows * D + h) - m);
+    l = fmaf(__ldcg(s + p.rows * D + p.rows + h), f, l);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = fmaf(__ldcg(s + h * D + d * 32 + lane), f, o[d]);
+  }
+}
+
+template <int D, int kFmt, int kNt, int kWpw>
+__global__ void __launch_bounds__(kThreads, 1) ssd_paged_decode_kernel(const __grid_constant__ PagedDecodeParams p) {
+  using G = Geo<D, kFmt>;
+  using W = Worker<D, kFmt, kNt>;
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ uint32_t s_pref[kThreads + 1];
+  __shared__ uint32_t s_warp[kWarps];
+  __shared__ int s_flag;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const PagedView& c = p.c;
+  const int n_vp = c.n_seqs * c.H * p.qt;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+
+  // ---- the stream of tiles: sums over runs of (sequence, head, group), one run per thread
+  const int run = (n_vp + kThreads - 1) / kThreads;
+  const int lo = min(n_vp, tid * run), hi = min(n_vp, lo + run);
+  auto length_of = [&](int vp) {
+    const int pair = vp / p.qt;
+    return paged_length(c, pair / c.H, pair % c.H);
+  };
+  auto tiles_of = [&](int len) { return (uint32_t)(len + G::kTile - 1) / (uint32_t)G::kTile; };
+  uint32_t sum = 0u;
+#pragma unroll 4
+  for (int i = lo; i < hi; ++i) {
+    const int len = length_of(i);
+    sum += tiles_of(len);
+    if (len == 0 && i % gridDim.x == blockIdx.x) {           // nothing held: zeros, and no weight anywhere
+      const int pair = i / p.qt, qi = i % p.qt, seq = pair / c.H, head = pair % c.H;
+      for (int h = qi * p.rows; h < min(p.g, (qi + 1) * p.rows); ++h) {
+        const long long qh = (long long)head * p.g + h;
+        for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + seq * p.o_seq + qh * p.o_head + 2 * d) = make_uint4(0u, 0u, 0u, 0u);
+        W::write_stats(p, seq, qh, kNegBig, 0.f);
+      }
+    }
+  }
+  uint32_t inc = sum;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, inc, s);
+    if (lane >= s) inc += x;
+  }
+  if (lane == 31) s_warp[warp] = inc;
+  __syncthreads();
+  uint32_t before = 0u, total = 0u;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += s_warp[w];
+    total += s_warp[w];
+  }
+  s_pref[tid] = before + inc - sum;
+  __syncthreads();
+
+  const uint32_t workers = gridDim.x * (kWarps / kWpw);
+  const uint32_t worker = kWpw == 1 ? blockIdx.x * kWarps + warp : blockIdx.x;
+  uint32_t share = (total + workers - 1) / workers;
+  if (share < (uint32_t)kWpw) share = kWpw;                  // a tile for every warp of the worker
+  const uint32_t first = worker * share, end = min(total, first + share);
+  if (first >= end) return;
+
+  // ---- the head that holds the worker's first tile
+  int vp;
+  uint32_t at;                                               // tiles before vp
+  {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) n += s_pref[i * 32 + lane] <= first;
+    n = __reduce_add_sync(0xffffffffu, n);                   // runs that begin at or before it: the last of them has it
+    vp = (n - 1) * run;
+    at = s_pref[n - 1];
+    for (;;) {                                               // ends: `first` lies inside this run
+      const uint32_t mine = vp + lane < n_vp ? tiles_of(length_of(vp + lane)) : 0u;
+      uint32_t x = mine;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, s);
+        if (lane >= s) x += y;
+      }
+      const unsigned over = __ballot_sync(0xffffffffu, at + x > first);
+      if (over) {
+        const int who = __ffs(over) - 1;
+        at += __shfl_sync(0xffffffffu, x - mine, who);
+        vp += who;
+        break;
+      }
+      at += __shfl_sync(0xffffffffu, x, 31);
+      vp += 32;
+      if (vp >= n_vp) return;                                // cannot be: the tile exists
+    }
+  }
+
+  W w(p, lane, ring + warp * G::kRing);
+  const int part_floats = p.rows * (D + 2);
+  auto partial_of = [&](uint32_t who, bool starts) { return p.partial + ((size_t)who * 2 + (starts ? 1 : 0)) * part_floats; };
+  // the first tile of the worker's part of the head that holds tile g of the stream
+  auto enter = [&](Place& pl, int v, uint32_t start) {
+    pl.vp = v;
+    pl.len = length_of(v);
+    const uint32_t n = tiles_of(pl.len);
+    pl.t = first > start ? (int)(first - start) : 0;
+    pl.end = (int)min(n, end - start);
+  };
+  // Ends a head (or this worker's piece of it).  kWpw == 1: by the warp.  Returns whether the state was written out.
+  auto merge_pieces = [&](int v, uint32_t start, uint32_t n_tiles, int h0, int h_step) {
+    const uint32_t w0 = start / share, w1 = (start + n_tiles - 1) / share;
+    const int pair = v / p.qt, qi = v % p.qt, seq = pair / c.H, head = pair % c.H;
+    const int n_q = min(p.g - qi * p.rows, p.rows);
+    for (int h = h0; h < n_q; h += h_step) {
+      float o[D / 32], m, l;
+      merge_head<D>(p, lane, h, (int)(w1 - w0 + 1), [&](int i) { return (const float*)partial_of(w0 + i, i == 0); }, o, m, l);
+      const long long qh = (long long)head * p.g + qi * p.rows + h;
+      const float by = l > 0.f ? 1.f / l : l;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) store16(p.out + seq * p.o_seq + qh * p.o_head + 2 * (d * 32 + lane), o[d] * by, p.bf16 != 0);
+      if (lane == 0) W::write_stats(p, seq, qh, m, l);
+    }
+  };
+
+  constexpr int kStages = G::kStages;
+  if constexpr (kWpw == 1) {
+    // one stream of tiles per warp, across heads: `ahead` issues copies, `now` consumes
+    uint32_t n_issue = first, start_a = at, start_n = at;
+    Place ahead, now;
+    typename W::Rows rows;
+    enter(ahead, vp, start_a);
+    now = ahead;
+    int seq_a, head_a, qi_a;
+    auto name = [&](int v, int& seq, int& head, int& qi) {
+      const int pair = v / p.qt;
+      qi = v - pair * p.qt;
+      seq = pair / c.H;
+      head = pair - seq * c.H;
+    };
+    name(ahead.vp, seq_a, head_a, qi_a);
+    w.look_up(ahead, seq_a, head_a, rows);
+    auto advance = [&](Place& pl, uint32_t& start) {         // to the next tile; true: it is another head's
+      if (++pl.t < pl.end) return false;
+      do {
+        start += tiles_of(pl.len);
+        enter(pl, pl.vp + 1, start);
+      } while (pl.len == 0);
+      return true;
+    };
+    auto issue_next = [&](int stage) {
+      if (n_issue < end) {
+        w.issue(ahead, seq_a, head_a, qi_a, stage, rows);
+        if (++n_issue < end) {
+          if (advance(ahead, start_a)) name(ahead.vp, seq_a, head_a, qi_a);
+          w.look_up(ahead, seq_a, head_a, rows);
+        }
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) issue_next(s);
+    int stage = 0, seq, head, qi;
+    name(now.vp, seq, head, qi);
+    w.begin(seq, head, qi);
+    for (uint32_t i = first; i < end; ++i) {
+      cp_wait<kStages - 2>();
+      __syncwarp();
+      issue_next(stage == 0 ? kStages - 1 : stage - 1);
+      w.consume(now, seq, head, qi, stage);
+      __syncwarp();
+      if (++stage == kStages) stage = 0;
+      if (now.t + 1 == now.end) {
+        w.close();
+        const uint32_t n_tiles = tiles_of(now.len);
+        const uint32_t w0 = start_n / share, w1 = (start_n + n_tiles - 1) / share;
+        if (w0 == w1) {
+          w.write_out(seq, head, qi);
+        } else {
+          w.write_state(partial_of(worker, worker == w0), min(p.g - qi * p.rows, p.rows));
+          __threadfence();
+          __syncwarp();
+          uint32_t done = 0u;
+          if (lane == 0) done = atomicAdd(p.counters + w0, 1u);
+          done = __shfl_sync(0xffffffffu, done, 0);
+          if (done == w1 - w0) {
+            __threadfence();
+            if (lane == 0) p.counters[w0] = 0u;
+            merge_pieces(now.vp, start_n, n_tiles, 0, 1);
+          }
+        }
+      }
+      if (i + 1 < end && advance(now, start_n)) {
+        name(now.vp, seq, head, qi);
+        w.begin(seq, head, qi);
+      }
+    }
+  } else {
+    uint32_t done_to = first;
+    Place pl;
+    uint32_t start = at;
+    enter(pl, vp, start);
+    for (;;) {
+      const int pair = pl.vp / p.qt, qi = pl.vp % p.qt, seq = pair / c.H, head = pair % c.H;
+      const int n_q = min(p.g - qi * p.rows, p.rows);
+      const uint32_t n_tiles = tiles_of(pl.len);
+      const int t0 = pl.t, t1 = pl.end;
+      Place ahead = pl, now = pl;
+      ahead.t = now.t = t0 + warp;
+      typename W::Rows rows;
+      if (ahead.t < t1) w.look_up(ahead, seq, head, rows);
+      auto issue_next = [&](int stage) {
+        if (ahead.t < t1) {
+          w.issue(ahead, seq, head, qi, stage, rows);
+          ahead.t += kWarps;
+          if (ahead.t < t1) w.look_up(ahead, seq, head, rows);
+        }
+        cp_commit();
+      };
+#pragma unroll
+      for (int s = 0; s < kStages - 1; ++s) issue_next(s);
+      w.begin(seq, head, qi);
+      int stage = 0;
+      for (; now.t < t1; now.t += kWarps) {
+        cp_wait<kStages - 2>();
+        __syncwarp();
+        issue_next(stage == 0 ? kStages - 1 : stage - 1);
+        w.consume(now, seq, head, qi, stage);
+        __syncwarp();
+        if (++stage == kStages) stage = 0;
+      }
+      cp_wait<0>();
+      w.close();
+      // the warps' states, in their own rings (drained by now), merged by all of them
+      float* mine = reinterpret_cast<float*>(ring + warp * G::kRing);
+      __syncwarp();
+      w.write_state(mine, n_q);
+      __syncthreads();
+      const uint32_t w0 = start / share, w1 = (start + n_tiles - 1) / share;
+      const int n_states = min(kWarps, t1 - t0);
+      for (int h = warp; h < n_q; h += kWarps) {
+        float o[D / 32], m = kNegBig, l = 0.f;
+        for (int i = 0; i < n_states; ++i) m = fmaxf(m, reinterpret_cast<const float*>(ring + i * G::kRing)[p.rows * D + h]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] = 0.f;
+        for (int i = 0; i < n_states; ++i) {
+          const float* s = reinterpret_cast<const float*>(ring + i * G::kRing);
+          const float f = ex2(s[p.rows * D + h] - m);
+          l = fmaf(s[p.rows * D + p.rows + h], f, l);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) o[d] = fmaf(s[h * D + d * 32 + lane], f, o[d]);
+        }
+        if (w0 == w1) {
+          const long long qh = (long long)head * p.g + qi * p.rows + h;
+          const float by = l > 0.f ? 1.f / l : l;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) store16(p.out + seq * p.o_seq + qh * p.o_head + 2 * (d * 32 + lane), o[d] * by, p.bf16 != 0);
+          if (lane == 0) W::write_stats(p, seq, qh, m, l);
+        } else {
+          float* to = partial_of(worker, worker == w0);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) to[h * D + d * 32 + lane] = o[d];
+          if (lane == 0) {
+            to[p.rows * D + h] = m;
+            to[p.rows * D + p.rows + h] = l;
+          }
+        }
+      }
+      if (w0 != w1) {
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+          const uint32_t done = atomicAdd(p.counters + w0, 1u);
+          s_flag = done == w1 - w0;
+          if (s_flag) p.counters[w0] = 0u;
+        }
+        __syncthreads();
+        if (s_flag) {
+          __threadfence();
+          merge_pieces(pl.vp, start, n_tiles, warp, kWarps);
+        }
+      }
+      done_to += t1 - t0;
+      if (done_to >= end) break;
+      do {
+        start += tiles_of(pl.len);
+        enter(pl, pl.vp + 1, start);
+      } while (pl.len == 0);
+      __syncthreads();                                       // the rings are free again, and s_flag
+    }
+  }
+}
+
+template <int D, int kFmt, int kNt, int kWpw>
+cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_t st) {
+  using G = Geo<D, kFmt>;
+  auto* kernel = ssd_paged_decode_kernel<D, kFmt, kNt, kWpw>;
+  // once per device; host threads that meet here make the same idempotent call
+  static std::atomic<bool> ready[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready[dev].store(true, std::memory_order_release);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sms);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = G::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, kernel, p);
+  count_launch();
+  return e;
+}
+
+template <int D, int kFmt>
+cudaError_t launch_paged_format(const PagedDecodeParams& p, int sms, cudaStream_t st) {
+  // Many heads: a warp per share, and no meeting of warps.  Few heads: a thread block per share, so that a head's
+  // pieces to be merged through memory are at most one per thread block.
+  const bool many = (long long)p.c.n_seqs * p.c.H * p.qt >= 2ll * sms;
+  if (p.rows <= 8) return many ? launch_paged_kernel<D, kFmt, 1, 1>(p, sms, st) : launch_paged_kernel<D, kFmt, 1, kWarps>(p, sms, st);
+  return many ? launch_paged_kernel<D, kFmt, 2, 1>(p, sms, st) : launch_paged_kernel<D, kFmt, 2, kWarps>(p, sms, st);
+}
+
+}  // namespace paged
+}  // namespace ssd
