@@ -437,7 +437,7 @@ Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate,
   const size_t heads = (size_t)v.n_seqs * v.H * g;
   Workspace w;
   w.partial = align_up(paged_max_workers(sms) * 4);
-  w.ml = align_up(w.partial + paged_max_workers(sms) * 2 * rows * (head_dim + 2) * 4);
+  w.ml = align_up(w.partial + paged_max_workers(sms) * 2 * paged_part_floats(rows, head_dim) * 4);
   w.logits = align_up(w.ml + (accumulate ? heads * 8 : 0));
   w.bytes = w.logits + (accumulate ? heads * (size_t)v.cap * 4 : 0);
   return w;
@@ -463,6 +463,8 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   p.g = a->n_q_heads / kv->n_kv_heads;
   p.rows = paged_rows(p.g);
   p.qt = (p.g + p.rows - 1) / p.rows;
+  p.by_qt = fast_div((uint32_t)p.qt);
+  p.by_heads = fast_div((uint32_t)kv->n_kv_heads);
   // tiles are counted in 32 bits (a tile has 16 slots at least)
   if ((double)kv->n_seqs * kv->n_kv_heads * p.qt * (p.c.cap / 16 + 1) > 2.0e9) return SSD_ERR_LIMIT;
   if (kv->n_seqs == 0) return SSD_OK;

@@ -113,6 +113,21 @@ __device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, flo
 #endif
 
 // ------------------------------------------------------------------ attention of one new token
+// n / d for n < 2^31 by a multiplication (the round-up method of Granlund and Montgomery, PLDI 1994: with s = ceil(log2 d)
+// and m = floor(2^32 (2^s - d) / d) + 1, the quotient is (n + floor(m n / 2^32)) >> s)
+struct FastDiv {
+  uint32_t m, s;
+#if defined(__CUDACC__)
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return (n + __umulhi(n, m)) >> s; }
+#endif
+};
+inline FastDiv fast_div(uint32_t d) {
+  FastDiv f = {0u, 0u};
+  while ((1ull << f.s) < d) ++f.s;
+  f.m = (uint32_t)(((1ull << 32) * ((1ull << f.s) - d)) / d + 1u);
+  return f;
+}
+
 struct PagedDecodeParams {
   PagedView c;
   const char* q;            // [n_seqs, H * g, D], strides in bytes
@@ -127,9 +142,11 @@ struct PagedDecodeParams {
   float2* ml;               // weights wanted: [n_seqs * H * g] (max, sum)
   long long logit_row;
   uint32_t* counters;       // [workers], zero between launches
-  float* partial;           // [workers][2][rows * (D + 2)]
+  float* partial;           // [workers][2][paged_part_floats(rows, D)]
   float scale_log2;
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together
+  FastDiv by_qt, by_heads;  // n / qt, n / H
+  int whole_tiles;          // the page size is a multiple of the tile's slots
   int bf16;                 // type of q, out, k_new, v_new: 1 bf16, 0 fp16
 };
 
@@ -137,6 +154,12 @@ enum { kPagedBf16 = 0, kPagedFp16 = 1, kPagedE4m3 = 2 };
 
 // query heads that one pass over a key head's rows serves
 inline int paged_rows(int g) { return g < 16 ? g : 16; }
+
+// a state in memory: O [rows][D], m [rows], l [rows], whole float4s
+#if defined(__CUDACC__)
+__host__ __device__
+#endif
+inline int paged_part_floats(int rows, int head_dim) { return (rows * (head_dim + 2) + 3) / 4 * 4; }
 
 cudaError_t launch_paged_decode_16(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st);
 cudaError_t launch_paged_decode_8(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st);

@@ -3,7 +3,7 @@
 
 namespace ssd {
 
-size_t paged_max_workers(int sms) { return (size_t)sms * paged::kWarps; }
+size_t paged_max_workers(int sms) { return (size_t)sms * 16; }
 
 cudaError_t launch_paged_decode_16(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st) {
   if (p.bf16)

@@ -6,7 +6,7 @@
 //
 // Work: the slots of a key head are cut into tiles of 8 KB (4 KB of K, 4 KB of V).  The tiles of all (sequence, head,
 // group) are one stream, cut into equal shares, one per worker, from the lengths that the launch finds on the device.
-// A worker is one warp (kWpw = 1), or the 8 warps of a thread block (kWpw = 8), which take a head's tiles in turn and
+// A worker is one warp, or all warps of a thread block (kCta), which take a head's tiles in turn and
 // merge their states in shared memory.  Heads cut by a share's border leave (O, m, l) of each piece in global memory;
 // whoever completes the last piece (a counter, kept under the worker that has the head's first piece: a worker has at
 // most one head that starts in its share and is cut at its end) merges them in the order of the workers: the result does not
@@ -34,13 +34,24 @@
 namespace ssd {
 namespace paged {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr float kShift = 14.f;
 constexpr float kNegInf = -__builtin_huge_valf();
 
-template <int D, int kFmt>
+#ifndef SSD_PAGED_FEW
+#define SSD_PAGED_FEW 256
+#endif
+constexpr int kPagedFewHeads = SSD_PAGED_FEW;   // not above the threads of a thread block
+#ifndef SSD_PAGED_WARPS1
+#define SSD_PAGED_WARPS1 12
+#define SSD_PAGED_STAGES1 2
+#define SSD_PAGED_WARPS2 8
+#define SSD_PAGED_STAGES2 3
+#endif
+template <int D, int kFmt, int kNt>
 struct Geo {
+  static constexpr int kWarps = kNt == 1 ? SSD_PAGED_WARPS1 : SSD_PAGED_WARPS2;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kStages = kNt == 1 ? SSD_PAGED_STAGES1 : SSD_PAGED_STAGES2;
   static constexpr int kRow = kFmt == kPagedE4m3 ? D : 2 * D;      // bytes of a row in a page
   static constexpr int kTile = 4096 / kRow;                        // keys of a tile
   static constexpr int kCpr = kRow / 16;                           // 16-byte chunks of a row
@@ -48,7 +59,6 @@ struct Geo {
   static constexpr int kScaleBytes = kFmt == kPagedE4m3 ? kTile * 8 : 0;
   static constexpr int kMaskAt = 8192 + kScaleBytes;               // 2 words: which rows exist
   static constexpr int kStage = (kMaskAt + 8 + 127) / 128 * 128;
-  static constexpr int kStages = 3;
   static constexpr int kRing = kStage * kStages;
   static constexpr int kSmem = kRing * kWarps;
 };
@@ -123,6 +133,8 @@ __device__ __forceinline__ void store16(char* to, float x, bool bf16) {
     *reinterpret_cast<__half*>(to) = __float2half_rn(x);
 }
 
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }   // no row at all: zeros (a NaN stays one)
+
 // A place in the stream of tiles.
 struct Place {
   int vp;        // (sequence * H + head) * qt + group
@@ -132,7 +144,7 @@ struct Place {
 
 template <int D, int kFmt, int kNt>
 struct Worker {
-  using G = Geo<D, kFmt>;
+  using G = Geo<D, kFmt, kNt>;
   static constexpr bool kBf16 = kFmt == kPagedBf16;        // type of the products' operands
   static constexpr int kKs = D / 16;
   const PagedDecodeParams& p;
@@ -231,6 +243,12 @@ struct Worker {
   };
   __device__ __forceinline__ void look_up(const Place& at, int seq, int head, Rows& r) const {
     const int32_t* table = paged_table(p.c, seq, head);
+    if (p.whole_tiles) {
+      int index;
+      paged_split(p.c, at.t * G::kTile, index, r.row[0]);
+      r.page[0] = __ldg(table + index);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < G::kRpl; ++i) {
       const int local = i * 32 + lane;
@@ -256,6 +274,58 @@ struct Worker {
     const PagedView& c = p.c;
     const bool fused = p.k_new != nullptr;
     const int last = at.len - 1 - at.t * G::kTile;           // the new row's place in this tile, if it is in it
+    constexpr int kRpi = 32 / G::kCpr;                       // rows that one copy instruction of the warp brings
+    const int chunk = lane % G::kCpr;
+    if (p.whole_tiles) {                                     // a tile lies in one page: one address, and strides
+      const bool ok = (uint32_t)r.page[0] < (uint32_t)c.n_pages;             // the same for the whole warp
+      if (!ok) paged_flag(c, kPagedBadPage);
+      const long long first = ok ? r.page[0] * c.page_b + head * c.head_b + r.row[0] * c.slot_b : 0;
+      const int skip = fused && last < G::kTile ? last : G::kTile;           // rows from here on are not copied ..
+      const int held = min(last + 1, G::kTile);                              // .. and rows from here on do not exist
+      const char* k = c.k + first + (lane / G::kCpr) * c.slot_b + chunk * 16;
+      const long long dv = c.v - c.k;
+      if (ok && skip == G::kTile && held == G::kTile) {
+#pragma unroll
+        for (int it = 0; it < G::kTile / kRpi; ++it) {
+          const uint32_t to = base + chunk_at(it * kRpi + lane / G::kCpr, chunk);
+          cp16(to, k, true);
+          cp16(to + 4096, k + dv, true);
+          k += kRpi * c.slot_b;
+        }
+      } else {
+#pragma unroll
+        for (int it = 0; it < G::kTile / kRpi; ++it) {
+          const int row = it * kRpi + lane / G::kCpr;
+          const uint32_t to = base + chunk_at(row, chunk);
+          const bool have = ok && row < held;
+          if (row != skip) {
+            cp16(to, have ? k : c.k, have);
+            cp16(to + 4096, have ? k + dv : c.v, have);
+          }
+          k += kRpi * c.slot_b;
+        }
+      }
+      if constexpr (kFmt == kPagedE4m3) {
+        const long long so = ok ? r.page[0] * c.sc_page + head * c.sc_head + r.row[0] * c.sc_slot : 0;
+#pragma unroll
+        for (int i = 0; i < G::kRpl; ++i) {
+          const int local = i * 32 + lane;
+          if (local < G::kTile && local != skip) {
+            const bool have = ok && local < held;
+            const long long at_s = have ? so + local * c.sc_slot : 0;
+            cp4(base + 8192 + local * 4, c.ks + at_s, have);
+            cp4(base + 8192 + G::kTile * 4 + local * 4, c.vs + at_s, have);
+          }
+        }
+      }
+      if (skip < G::kTile) put_new(at, seq, head, qi, base, last, r.page[0], r.row[0] + last);
+      if (lane == 0) {
+        uint2* mask = reinterpret_cast<uint2*>(ring_ptr + stage * G::kStage + G::kMaskAt);
+        const uint32_t lo = held >= 32 ? ~0u : (1u << held) - 1u, hi = held <= 32 ? 0u : (held >= 64 ? ~0u : (1u << (held - 32)) - 1u);
+        *mask = ok ? make_uint2(lo, hi) : make_uint2(0u, 0u);
+      }
+      return;
+    }
     long long off[G::kRpl];
     uint32_t have[2] = {0u, 0u};
 #pragma unroll
@@ -274,8 +344,6 @@ struct Worker {
         }
       }
     }
-    constexpr int kRpi = 32 / G::kCpr;                       // rows that one copy instruction of the warp brings
-    const int chunk = lane % G::kCpr;
 #pragma unroll
     for (int it = 0; it < G::kTile / kRpi; ++it) {
       const int row = it * kRpi + lane / G::kCpr;
@@ -287,7 +355,14 @@ struct Worker {
         cp16(to + 4096, c.v + from, f >= 0);
       }
     }
-    if (fused && last >= 0 && last < G::kTile) put_new(at, seq, head, qi, base, last, r);
+    if (fused && last < G::kTile) {
+      const int who = last / 32;
+      int page = r.page[0], row = r.row[0];
+#pragma unroll
+      for (int i = 1; i < G::kRpl; ++i)
+        if (who == i) page = r.page[i], row = r.row[i];
+      put_new(at, seq, head, qi, base, last, __shfl_sync(0xffffffffu, page, last & 31), __shfl_sync(0xffffffffu, row, last & 31));
+    }
     if (lane == 0) {
       uint32_t* mask = reinterpret_cast<uint32_t*>(ring_ptr + stage * G::kStage + G::kMaskAt);
       mask[0] = have[0];
@@ -297,15 +372,13 @@ struct Worker {
 
   // The rows of the token being appended: from k_new and v_new into the stage and, by the first group's worker, into
   // their page.  Nothing else of this launch reads that slot.
-  __device__ __noinline__ void put_new(const Place& at, int seq, int head, int qi, uint32_t base, int last, const Rows& r) {
+  __device__ __noinline__ void put_new(const Place& at, int seq, int head, int qi, uint32_t base, int last, int page, int row) {
     const PagedView& c = p.c;
     constexpr int kL = D / 8;                                // lanes that hold a row, 8 values each; V from lane 16 on
     const int part = lane & 15;
     const bool mine = part < kL;
     const char* from = (lane < 16 ? p.k_new : p.v_new) + seq * p.new_seq + head * p.new_head;
     const uint4 raw = mine ? __ldg(reinterpret_cast<const uint4*>(from) + part) : make_uint4(0u, 0u, 0u, 0u);
-    const int page = __shfl_sync(0xffffffffu, r.page[last / 32], last & 31);
-    const int row = __shfl_sync(0xffffffffu, r.row[last / 32], last & 31);
     const bool ok = (uint32_t)page < (uint32_t)c.n_pages;
     const bool store = ok && qi == 0;
     const long long off = ok ? page * c.page_b + head * c.head_b + row * c.slot_b : 0;
@@ -338,7 +411,7 @@ struct Worker {
     constexpr int kSub = G::kTile / 16;
     const uint32_t base = ring + stage * G::kStage;
     const unsigned char* mem = ring_ptr + stage * G::kStage;
-    float s[kSub][kNt][4];
+    float s[kSub][kNt][4], s2[kSub][kNt][4];                 // two sums, so that a product need not wait for the one before
     float vinv[kSub][2], vman[kSub][2];                      // 2^-e, and the V scale times that
     const int j8 = lane >> 2, mi = lane >> 3, ml8 = lane & 7;
 #pragma unroll
@@ -346,7 +419,7 @@ struct Worker {
 #pragma unroll
       for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[sb][nt][i] = 0.f;
+        for (int i = 0; i < 4; ++i) s[sb][nt][i] = s2[sb][nt][i] = 0.f;
       const int krow = sb * 16 + (mi & 1) * 8 + ml8;         // keys of matrix mi: halves alternate, then chunks
       if constexpr (kFmt == kPagedE4m3) {
 #pragma unroll
@@ -357,7 +430,7 @@ struct Worker {
           for (int u = 0; u < 2; ++u) {
             const uint32_t a[4] = {widen_lo(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u]), widen_hi(r[2 * u + 1])};
 #pragma unroll
-            for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(s[sb][nt], a, qf[nt][2 * c2 + u]);
+            for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(u == 0 ? s[sb][nt] : s2[sb][nt], a, qf[nt][2 * c2 + u]);
           }
         }
       } else {
@@ -366,7 +439,7 @@ struct Worker {
           uint32_t a[4];
           ldsm4(a, base + chunk_at(krow, 2 * ks + (mi >> 1)));
 #pragma unroll
-          for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(s[sb][nt], a, qf[nt][ks]);
+          for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(ks % 2 == 0 ? s[sb][nt] : s2[sb][nt], a, qf[nt][ks]);
         }
       }
     }
@@ -384,6 +457,7 @@ struct Worker {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float& x = s[sb][nt][2 * hf + e];
+            x += s2[sb][nt][2 * hf + e];
             x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kNegInf;
           }
       }
@@ -530,7 +604,7 @@ struct Worker {
       }
   }
 
-  __device__ __forceinline__ void write_state(float* to, int n_q) const {    // [rows][D], then m[rows], l[rows]
+  __device__ __forceinline__ void write_state(float* to, int stride, int n_q) const {    // [rows][stride], then m[rows], l[rows]
 #pragma unroll
     for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
@@ -539,12 +613,12 @@ struct Worker {
         if (h < n_q) {
 #pragma unroll
           for (int mt = 0; mt < kKs; ++mt) {
-            to[h * D + dim_of(mt, 0)] = o[nt][mt][e];
-            to[h * D + dim_of(mt, 1)] = o[nt][mt][2 + e];
+            to[h * stride + dim_of(mt, 0)] = o[nt][mt][e];
+            to[h * stride + dim_of(mt, 1)] = o[nt][mt][2 + e];
           }
           if ((lane >> 2) == 0) {
-            to[p.rows * D + h] = m[nt][e];
-            to[p.rows * D + p.rows + h] = l[nt][e];
+            to[p.rows * stride + h] = m[nt][e];
+            to[p.rows * (stride + 1) + h] = l[nt][e];
           }
         }
       }
@@ -560,7 +634,7 @@ struct Worker {
         if (h < n_q) {
           const long long qh = (long long)head * p.g + qi * p.rows + h;
           char* to = p.out + seq * p.o_seq + qh * p.o_head;
-          const float by = l[nt][e] > 0.f ? 1.f / l[nt][e] : l[nt][e];       // no row at all: zeros (a NaN stays one)
+          const float by = inverse(l[nt][e]);
 #pragma unroll
           for (int mt = 0; mt < kKs; ++mt) {
             store16(to + 2 * dim_of(mt, 0), o[nt][mt][e] * by, p.bf16 != 0);
@@ -578,161 +652,181 @@ struct Worker {
   }
 };
 
-// Merge of n pieces of one query head, by a warp: piece(i) gives the state's memory (global: read past L1).
+// One query head's n pieces of one head, merged by a warp, in order: lane d4 < D / 4 ends with four sums (D == 64: lanes
+// 16 .. 31 hold the pieces of odd number until the end).  piece(i) is the memory of a state, read past L1.
 template <int D, class F>
-__device__ __forceinline__ void merge_head(const PagedDecodeParams& p, int lane, int h, int n, F piece, float (&o)[D / 32], float& m, float& l) {
+__device__ __forceinline__ void merge_head(const PagedDecodeParams& p, int lane, int h, int n, F piece, float4& o, float& m, float& l) {
+  constexpr int kGroups = 128 / D;
   m = kNegBig;
   for (int i = lane; i < n; i += 32) m = fmaxf(m, __ldcg(piece(i) + p.rows * D + h));
 #pragma unroll
   for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
   l = 0.f;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) o[d] = 0.f;
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float f = 0.f;
+    if (i0 + lane < n) {
+      f = ex2(__ldcg(piece(i0 + lane) + p.rows * D + h) - m);
+      l = fmaf(__ldcg(piece(i0 + lane) + p.rows * (D + 1) + h), f, l);
+    }
+    const int top = min(32, n - i0);
 #pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float* s = piece(i);
-    const float f = ex2(__ldcg(s + p.rows * D + h) - m);
-    l = fmaf(__ldcg(s + p.rows * D + p.rows + h), f, l);
+    for (int i = 0; i < top; i += kGroups) {
+      const int mine = i + lane / (D / 4);
+      const float by = __shfl_sync(0xffffffffu, f, mine);
+      if (mine < top) {
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(piece(i0 + mine) + h * D) + lane % (D / 4));
+        o.x = fmaf(x.x, by, o.x);
+        o.y = fmaf(x.y, by, o.y);
+        o.z = fmaf(x.z, by, o.z);
+        o.w = fmaf(x.w, by, o.w);
+      }
+    }
+  }
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) o[d] = fmaf(__ldcg(s + h * D + d * 32 + lane), f, o[d]);
+  for (int s = 16; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+  if constexpr (kGroups == 2) {
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
+    o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
+    o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
   }
 }
 
-template <int D, int kFmt, int kNt, int kWpw>
-__global__ void __launch_bounds__(kThreads, 1) ssd_paged_decode_kernel(const __grid_constant__ PagedDecodeParams p) {
-  using G = Geo<D, kFmt>;
+__device__ __forceinline__ void store4(char* to, const float4& x, float by, bool bf16) {
+  uint2 w;
+  if (bf16) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x * by, x.y * by), b = __floats2bfloat162_rn(x.z * by, x.w * by);
+    memcpy(&w.x, &a, 4);
+    memcpy(&w.y, &b, 4);
+  } else {
+    const __half2 a = __floats2half2_rn(x.x * by, x.y * by), b = __floats2half2_rn(x.z * by, x.w * by);
+    memcpy(&w.x, &a, 4);
+    memcpy(&w.y, &b, 4);
+  }
+  *reinterpret_cast<uint2*>(to) = w;
+}
+template <int kThreads>
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uint32_t& total) {   // exclusive sum
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t inc = x;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, inc, s);
+    if (lane >= s) inc += y;
+  }
+  if (lane == 31) s_warp[warp] = inc;
+  __syncthreads();
+  uint32_t before = 0u;
+  total = 0u;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    const uint32_t y = s_warp[w];
+    if (w < warp) before += y;
+    total += y;
+  }
+  __syncthreads();
+  return before + inc - x;
+}
+
+template <int D, int kFmt, int kNt, bool kCta>
+__global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_decode_kernel(const __grid_constant__ PagedDecodeParams p) {
+  using G = Geo<D, kFmt, kNt>;
   using W = Worker<D, kFmt, kNt>;
+  constexpr int kWarps = G::kWarps, kThreads = G::kThreads, kStages = G::kStages;
   extern __shared__ __align__(128) unsigned char ring[];
-  __shared__ uint32_t s_pref[kThreads + 1];
+  __shared__ uint32_t s_pref[kThreads];
   __shared__ uint32_t s_warp[kWarps];
-  __shared__ int s_flag;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& c = p.c;
   const int n_vp = c.n_seqs * c.H * p.qt;
   pdl_wait_predecessor();
   pdl_allow_successor();
 
-  // ---- the stream of tiles: sums over runs of (sequence, head, group), one run per thread
-  const int run = (n_vp + kThreads - 1) / kThreads;
-  const int lo = min(n_vp, tid * run), hi = min(n_vp, lo + run);
-  auto length_of = [&](int vp) {
-    const int pair = vp / p.qt;
-    return paged_length(c, pair / c.H, pair % c.H);
+  auto name = [&](int v, int& seq, int& head, int& qi) {
+    const uint32_t pair = p.by_qt.div((uint32_t)v);
+    qi = v - (int)pair * p.qt;
+    seq = (int)p.by_heads.div(pair);
+    head = (int)pair - seq * c.H;
+  };
+  auto length_of = [&](int v) {
+    int seq, head, qi;
+    name(v, seq, head, qi);
+    return paged_length(c, seq, head);
   };
   auto tiles_of = [&](int len) { return (uint32_t)(len + G::kTile - 1) / (uint32_t)G::kTile; };
-  uint32_t sum = 0u;
-#pragma unroll 4
-  for (int i = lo; i < hi; ++i) {
-    const int len = length_of(i);
-    sum += tiles_of(len);
-    if (len == 0 && i % gridDim.x == blockIdx.x) {           // nothing held: zeros, and no weight anywhere
-      const int pair = i / p.qt, qi = i % p.qt, seq = pair / c.H, head = pair % c.H;
-      for (int h = qi * p.rows; h < min(p.g, (qi + 1) * p.rows); ++h) {
-        const long long qh = (long long)head * p.g + h;
-        for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + seq * p.o_seq + qh * p.o_head + 2 * d) = make_uint4(0u, 0u, 0u, 0u);
-        W::write_stats(p, seq, qh, kNegBig, 0.f);
-      }
+  auto zeros = [&](int v) {                                  // nothing held: zeros, and no weight anywhere
+    int seq, head, qi;
+    name(v, seq, head, qi);
+    for (int h = qi * p.rows; h < min(p.g, (qi + 1) * p.rows); ++h) {
+      const long long qh = (long long)head * p.g + h;
+      for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + seq * p.o_seq + qh * p.o_head + 2 * d) = make_uint4(0u, 0u, 0u, 0u);
+      W::write_stats(p, seq, qh, kNegBig, 0.f);
     }
-  }
-  uint32_t inc = sum;
-#pragma unroll
-  for (int s = 1; s < 32; s <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, inc, s);
-    if (lane >= s) inc += x;
-  }
-  if (lane == 31) s_warp[warp] = inc;
-  __syncthreads();
-  uint32_t before = 0u, total = 0u;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += s_warp[w];
-    total += s_warp[w];
-  }
-  s_pref[tid] = before + inc - sum;
-  __syncthreads();
-
-  const uint32_t workers = gridDim.x * (kWarps / kWpw);
-  const uint32_t worker = kWpw == 1 ? blockIdx.x * kWarps + warp : blockIdx.x;
-  uint32_t share = (total + workers - 1) / workers;
-  if (share < (uint32_t)kWpw) share = kWpw;                  // a tile for every warp of the worker
-  const uint32_t first = worker * share, end = min(total, first + share);
-  if (first >= end) return;
-
-  // ---- the head that holds the worker's first tile
-  int vp;
-  uint32_t at;                                               // tiles before vp
-  {
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) n += s_pref[i * 32 + lane] <= first;
-    n = __reduce_add_sync(0xffffffffu, n);                   // runs that begin at or before it: the last of them has it
-    vp = (n - 1) * run;
-    at = s_pref[n - 1];
-    for (;;) {                                               // ends: `first` lies inside this run
-      const uint32_t mine = vp + lane < n_vp ? tiles_of(length_of(vp + lane)) : 0u;
-      uint32_t x = mine;
-#pragma unroll
-      for (int s = 1; s < 32; s <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, x, s);
-        if (lane >= s) x += y;
-      }
-      const unsigned over = __ballot_sync(0xffffffffu, at + x > first);
-      if (over) {
-        const int who = __ffs(over) - 1;
-        at += __shfl_sync(0xffffffffu, x - mine, who);
-        vp += who;
-        break;
-      }
-      at += __shfl_sync(0xffffffffu, x, 31);
-      vp += 32;
-      if (vp >= n_vp) return;                                // cannot be: the tile exists
-    }
-  }
-
-  W w(p, lane, ring + warp * G::kRing);
-  const int part_floats = p.rows * (D + 2);
+  };
+  const int part_floats = paged_part_floats(p.rows, D);
+  // a worker's pieces of heads that it shares: the one that starts in its share, and the one that does not
   auto partial_of = [&](uint32_t who, bool starts) { return p.partial + ((size_t)who * 2 + (starts ? 1 : 0)) * part_floats; };
-  // the first tile of the worker's part of the head that holds tile g of the stream
-  auto enter = [&](Place& pl, int v, uint32_t start) {
-    pl.vp = v;
-    pl.len = length_of(v);
-    const uint32_t n = tiles_of(pl.len);
-    pl.t = first > start ? (int)(first - start) : 0;
-    pl.end = (int)min(n, end - start);
-  };
-  // Ends a head (or this worker's piece of it).  kWpw == 1: by the warp.  Returns whether the state was written out.
-  auto merge_pieces = [&](int v, uint32_t start, uint32_t n_tiles, int h0, int h_step) {
-    const uint32_t w0 = start / share, w1 = (start + n_tiles - 1) / share;
-    const int pair = v / p.qt, qi = v % p.qt, seq = pair / c.H, head = pair % c.H;
-    const int n_q = min(p.g - qi * p.rows, p.rows);
-    for (int h = h0; h < n_q; h += h_step) {
-      float o[D / 32], m, l;
-      merge_head<D>(p, lane, h, (int)(w1 - w0 + 1), [&](int i) { return (const float*)partial_of(w0 + i, i == 0); }, o, m, l);
-      const long long qh = (long long)head * p.g + qi * p.rows + h;
-      const float by = l > 0.f ? 1.f / l : l;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) store16(p.out + seq * p.o_seq + qh * p.o_head + 2 * (d * 32 + lane), o[d] * by, p.bf16 != 0);
-      if (lane == 0) W::write_stats(p, seq, qh, m, l);
-    }
-  };
+  W w(p, lane, ring + warp * G::kRing);
+  auto steps = [&](int n) { return n > 0 ? n + kStages - 1 : 0; };
 
-  constexpr int kStages = G::kStages;
-  if constexpr (kWpw == 1) {
+  if constexpr (!kCta) {
+    // ---- the stream of tiles: sums over runs of (sequence, head, group), one run per thread
+    const int run = (n_vp + kThreads - 1) / kThreads;
+    const int lo = min(n_vp, tid * run), hi = min(n_vp, lo + run);
+    uint32_t sum = 0u, total;
+#pragma unroll 4
+    for (int i = lo; i < hi; ++i) {
+      const int len = length_of(i);
+      sum += tiles_of(len);
+      if (len == 0 && (uint32_t)i % gridDim.x == blockIdx.x) zeros(i);
+    }
+    s_pref[tid] = block_scan<kThreads>(sum, s_warp, total);
+    __syncthreads();
+    const uint32_t workers = gridDim.x * kWarps, worker = blockIdx.x * kWarps + warp;
+    uint32_t share = (total + workers - 1) / workers;
+    if (share == 0u) share = 1u;
+    const uint32_t first = worker * share, end = min(total, first + share);
+    if (first >= end) return;
+
+    // ---- the head that holds the worker's first tile
+    int vp;
+    uint32_t at;                                             // tiles before vp
+    {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kThreads / 32; ++i) n += s_pref[i * 32 + lane] <= first;
+      n = __reduce_add_sync(0xffffffffu, n);                 // runs that begin at or before it: the last of them has it
+      vp = (n - 1) * run;
+      at = s_pref[n - 1];
+      for (;;) {                                             // ends: `first` lies inside this run
+        const uint32_t mine = vp + lane < n_vp ? tiles_of(length_of(vp + lane)) : 0u;
+        uint32_t x = mine;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+          const uint32_t y = __shfl_up_sync(0xffffffffu, x, s);
+          if (lane >= s) x += y;
+        }
+        const unsigned over = __ballot_sync(0xffffffffu, at + x > first);
+        if (over) {
+          const int who = __ffs(over) - 1;
+          at += __shfl_sync(0xffffffffu, x - mine, who);
+          vp += who;
+          break;
+        }
+        at += __shfl_sync(0xffffffffu, x, 31);
+        vp += 32;
+        if (vp >= n_vp) return;                              // cannot be: the tile exists
+      }
+    }
     // one stream of tiles per warp, across heads: `ahead` issues copies, `now` consumes
-    uint32_t n_issue = first, start_a = at, start_n = at;
-    Place ahead, now;
-    typename W::Rows rows;
-    enter(ahead, vp, start_a);
-    now = ahead;
-    int seq_a, head_a, qi_a;
-    auto name = [&](int v, int& seq, int& head, int& qi) {
-      const int pair = v / p.qt;
-      qi = v - pair * p.qt;
-      seq = pair / c.H;
-      head = pair - seq * c.H;
+    auto enter = [&](Place& pl, int v, uint32_t start) {     // the worker's part of a head whose first tile is `start`
+      pl.vp = v;
+      pl.len = length_of(v);
+      const uint32_t n = tiles_of(pl.len);
+      pl.t = first > start ? (int)(first - start) : 0;
+      pl.end = (int)min(n, end - start);
     };
-    name(ahead.vp, seq_a, head_a, qi_a);
-    w.look_up(ahead, seq_a, head_a, rows);
     auto advance = [&](Place& pl, uint32_t& start) {         // to the next tile; true: it is another head's
       if (++pl.t < pl.end) return false;
       do {
@@ -741,36 +835,43 @@ __global__ void __launch_bounds__(kThreads, 1) ssd_paged_decode_kernel(const __g
       } while (pl.len == 0);
       return true;
     };
-    auto issue_next = [&](int stage) {
-      if (n_issue < end) {
-        w.issue(ahead, seq_a, head_a, qi_a, stage, rows);
-        if (++n_issue < end) {
+    uint32_t start_a = at, start_n = at;
+    Place ahead, now;
+    typename W::Rows rows;
+    enter(ahead, vp, start_a);
+    now = ahead;
+    int seq_a, head_a, qi_a, seq, head, qi;
+    name(ahead.vp, seq_a, head_a, qi_a);
+    seq = seq_a; head = head_a; qi = qi_a;
+    w.look_up(ahead, seq_a, head_a, rows);
+    w.begin(seq, head, qi);
+    const int n = (int)(end - first);
+    int in = 0, out = 0;                                     // stages
+#pragma unroll 1
+    for (int i = 0; i < steps(n); ++i) {
+      if (i < n) {
+        w.issue(ahead, seq_a, head_a, qi_a, in, rows);
+        if (i + 1 < n) {
           if (advance(ahead, start_a)) name(ahead.vp, seq_a, head_a, qi_a);
           w.look_up(ahead, seq_a, head_a, rows);
         }
+        if (++in == kStages) in = 0;
       }
       cp_commit();
-    };
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) issue_next(s);
-    int stage = 0, seq, head, qi;
-    name(now.vp, seq, head, qi);
-    w.begin(seq, head, qi);
-    for (uint32_t i = first; i < end; ++i) {
-      cp_wait<kStages - 2>();
+      if (i < kStages - 1) continue;
+      cp_wait<kStages - 1>();
       __syncwarp();
-      issue_next(stage == 0 ? kStages - 1 : stage - 1);
-      w.consume(now, seq, head, qi, stage);
+      w.consume(now, seq, head, qi, out);
       __syncwarp();
-      if (++stage == kStages) stage = 0;
+      if (++out == kStages) out = 0;
       if (now.t + 1 == now.end) {
         w.close();
-        const uint32_t n_tiles = tiles_of(now.len);
-        const uint32_t w0 = start_n / share, w1 = (start_n + n_tiles - 1) / share;
+        const uint32_t w0 = start_n / share, w1 = (start_n + tiles_of(now.len) - 1) / share;
+        const int n_q = min(p.g - qi * p.rows, p.rows);
         if (w0 == w1) {
           w.write_out(seq, head, qi);
         } else {
-          w.write_state(partial_of(worker, worker == w0), min(p.g - qi * p.rows, p.rows));
+          w.write_state(partial_of(worker, worker == w0), D, n_q);
           __threadfence();
           __syncwarp();
           uint32_t done = 0u;
@@ -779,115 +880,236 @@ __global__ void __launch_bounds__(kThreads, 1) ssd_paged_decode_kernel(const __g
           if (done == w1 - w0) {
             __threadfence();
             if (lane == 0) p.counters[w0] = 0u;
-            merge_pieces(now.vp, start_n, n_tiles, 0, 1);
+            for (int h = 0; h < n_q; ++h) {
+              float4 o;
+              float m, l;
+              merge_head<D>(p, lane, h, (int)(w1 - w0 + 1), [&](int k) { return (const float*)partial_of(w0 + k, k == 0); }, o, m, l);
+              const long long qh = (long long)head * p.g + qi * p.rows + h;
+              if (lane < D / 4) store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * lane, o, inverse(l), p.bf16 != 0);
+              if (lane == 0) W::write_stats(p, seq, qh, m, l);
+            }
           }
         }
       }
-      if (i + 1 < end && advance(now, start_n)) {
+      if (i < n + kStages - 2 && advance(now, start_n)) {
         name(now.vp, seq, head, qi);
         w.begin(seq, head, qi);
       }
     }
   } else {
-    uint32_t done_to = first;
-    Place pl;
-    uint32_t start = at;
-    enter(pl, vp, start);
-    for (;;) {
-      const int pair = pl.vp / p.qt, qi = pl.vp % p.qt, seq = pair / c.H, head = pair % c.H;
+    // ---- one (sequence, head, group) per thread (there are at most kThreads)
+    __shared__ int s_len[kThreads];
+    __shared__ int s_vp, s_last;
+    __shared__ float s_f[kWarps][16], s_m[16], s_l[16];
+    constexpr int kPad = D + 4;                              // row of a state in shared memory: no conflicts when it is written
+    int len = 0;
+    if (tid < n_vp) {
+      len = length_of(tid);
+      if (len == 0 && (uint32_t)tid % gridDim.x == blockIdx.x) zeros(tid);
+    }
+    s_len[tid] = len;
+    const uint32_t tiles = tiles_of(len);
+    uint32_t total;
+    uint32_t before = block_scan<kThreads>(tiles, s_warp, total);
+    const uint32_t n_held = (uint32_t)__syncthreads_count(len > 0);
+    if (total == 0u) return;
+    const uint32_t workers = gridDim.x, worker = blockIdx.x;
+    // Equal shares of the stream, which leave a worker with pieces of two heads, one after the other; or, where that
+    // costs little, whole pieces of one head each: pieces of `cut` tiles, of which there are at most `workers`.  A second
+    // piece costs a worker some 3 us (its first loads, and merging twice), the time of 16 tiles.
+    uint32_t share = max((total + workers - 1) / workers, (uint32_t)kWarps);
+    uint32_t cut = 0u;
+    if (n_held < workers) {
+      cut = max((total + workers - n_held - 1) / (workers - n_held), (uint32_t)kWarps);
+      if (cut > share + 16u) cut = 0u;
+    }
+    uint32_t first, end;
+    if (cut) {
+      const uint32_t pieces = (tiles + cut - 1) / cut;
+      uint32_t all;
+      before = block_scan<kThreads>(pieces, s_warp, all);
+      if (worker >= all) return;
+      if (before <= worker && worker < before + pieces) s_vp = tid;
+      first = end = 0u;
+    } else {
+      first = worker * share;
+      end = min(total, first + share);
+      if (first >= end) return;
+      if (before <= first && first < before + tiles) s_vp = tid;
+    }
+    s_pref[tid] = before;
+    __syncthreads();
+    for (int vp = s_vp;;) {
+      int seq, head, qi;
+      name(vp, seq, head, qi);
       const int n_q = min(p.g - qi * p.rows, p.rows);
-      const uint32_t n_tiles = tiles_of(pl.len);
-      const int t0 = pl.t, t1 = pl.end;
-      Place ahead = pl, now = pl;
-      ahead.t = now.t = t0 + warp;
+      Place pl;
+      pl.vp = vp;
+      pl.len = s_len[vp];
+      const uint32_t n_tiles = tiles_of(pl.len), start = s_pref[vp];
+      uint32_t w0, w1;                                       // the workers that share this head
+      int t0;
+      if (cut) {
+        w0 = start;
+        w1 = start + (n_tiles - 1) / cut;
+        t0 = (int)((worker - w0) * cut);
+        pl.end = (int)min(n_tiles, t0 + cut);
+      } else {
+        w0 = start / share;
+        w1 = (start + n_tiles - 1) / share;
+        t0 = first > start ? (int)(first - start) : 0;
+        pl.end = (int)min(n_tiles, end - start);
+      }
+      Place now = pl;
+      pl.t = now.t = t0 + warp;
+      const int n = pl.end > pl.t ? (pl.end - pl.t + kWarps - 1) / kWarps : 0;
       typename W::Rows rows;
-      if (ahead.t < t1) w.look_up(ahead, seq, head, rows);
-      auto issue_next = [&](int stage) {
-        if (ahead.t < t1) {
-          w.issue(ahead, seq, head, qi, stage, rows);
-          ahead.t += kWarps;
-          if (ahead.t < t1) w.look_up(ahead, seq, head, rows);
+      if (n > 0) w.look_up(pl, seq, head, rows);
+      w.begin(seq, head, qi);
+      int in = 0, out = 0;
+#pragma unroll 1
+      for (int i = 0; i < steps(n); ++i) {
+        if (i < n) {
+          w.issue(pl, seq, head, qi, in, rows);
+          pl.t += kWarps;
+          if (i + 1 < n) w.look_up(pl, seq, head, rows);
+          if (++in == kStages) in = 0;
         }
         cp_commit();
-      };
-#pragma unroll
-      for (int s = 0; s < kStages - 1; ++s) issue_next(s);
-      w.begin(seq, head, qi);
-      int stage = 0;
-      for (; now.t < t1; now.t += kWarps) {
-        cp_wait<kStages - 2>();
+        if (i < kStages - 1) continue;
+        cp_wait<kStages - 1>();
         __syncwarp();
-        issue_next(stage == 0 ? kStages - 1 : stage - 1);
-        w.consume(now, seq, head, qi, stage);
+        w.consume(now, seq, head, qi, out);
+        now.t += kWarps;
         __syncwarp();
-        if (++stage == kStages) stage = 0;
+        if (++out == kStages) out = 0;
       }
-      cp_wait<0>();
       w.close();
-      // the warps' states, in their own rings (drained by now), merged by all of them
-      float* mine = reinterpret_cast<float*>(ring + warp * G::kRing);
-      __syncwarp();
-      w.write_state(mine, n_q);
+      // ---- the warps' states meet in their own rings (which are drained), in the order of the warps
+      auto state = [&](int i) { return reinterpret_cast<const float*>(ring + i * G::kRing); };
+      w.write_state(reinterpret_cast<float*>(ring + warp * G::kRing), kPad, n_q);
+      const int n_states = min(kWarps, pl.end - t0);
       __syncthreads();
-      const uint32_t w0 = start / share, w1 = (start + n_tiles - 1) / share;
-      const int n_states = min(kWarps, t1 - t0);
       for (int h = warp; h < n_q; h += kWarps) {
-        float o[D / 32], m = kNegBig, l = 0.f;
-        for (int i = 0; i < n_states; ++i) m = fmaxf(m, reinterpret_cast<const float*>(ring + i * G::kRing)[p.rows * D + h]);
+        float m = lane < n_states ? state(lane)[p.rows * kPad + h] : kNegBig;
+        float l = lane < n_states ? state(lane)[p.rows * (kPad + 1) + h] : 0.f;
+        float top = m;
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[d] = 0.f;
-        for (int i = 0; i < n_states; ++i) {
-          const float* s = reinterpret_cast<const float*>(ring + i * G::kRing);
-          const float f = ex2(s[p.rows * D + h] - m);
-          l = fmaf(s[p.rows * D + p.rows + h], f, l);
+        for (int s = 8; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        const float f = ex2(m - top);
+        l *= f;
 #pragma unroll
-          for (int d = 0; d < D / 32; ++d) o[d] = fmaf(s[h * D + d * 32 + lane], f, o[d]);
-        }
-        if (w0 == w1) {
+        for (int s = 8; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+        if (lane < kWarps) s_f[lane][h] = f;
+        if (lane == 0) { s_m[h] = top; s_l[h] = l; }
+      }
+      __syncthreads();
+      const bool whole = w0 == w1;
+      float* part = partial_of(worker, worker == w0);
+      for (int col = tid; col < n_q * (D / 4); col += kThreads) {
+        const int h = col / (D / 4), d4 = col % (D / 4);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i)
+          if (i < n_states) {
+            const float4 x = *reinterpret_cast<const float4*>(state(i) + h * kPad + 4 * d4);
+            const float f = s_f[i][h];
+            o.x = fmaf(x.x, f, o.x);
+            o.y = fmaf(x.y, f, o.y);
+            o.z = fmaf(x.z, f, o.z);
+            o.w = fmaf(x.w, f, o.w);
+          }
+        if (whole) {
           const long long qh = (long long)head * p.g + qi * p.rows + h;
-          const float by = l > 0.f ? 1.f / l : l;
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) store16(p.out + seq * p.o_seq + qh * p.o_head + 2 * (d * 32 + lane), o[d] * by, p.bf16 != 0);
-          if (lane == 0) W::write_stats(p, seq, qh, m, l);
+          store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, inverse(s_l[h]), p.bf16 != 0);
+          if (d4 == 0) W::write_stats(p, seq, qh, s_m[h], s_l[h]);
         } else {
-          float* to = partial_of(worker, worker == w0);
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) to[h * D + d * 32 + lane] = o[d];
-          if (lane == 0) {
-            to[p.rows * D + h] = m;
-            to[p.rows * D + p.rows + h] = l;
+          __stcg(reinterpret_cast<float4*>(part + h * D) + d4, o);
+          if (d4 == 0) {
+            __stcg(part + p.rows * D + h, s_m[h]);
+            __stcg(part + p.rows * (D + 1) + h, s_l[h]);
           }
         }
       }
-      if (w0 != w1) {
+      if (!whole) {
         __threadfence();
         __syncthreads();
         if (tid == 0) {
           const uint32_t done = atomicAdd(p.counters + w0, 1u);
-          s_flag = done == w1 - w0;
-          if (s_flag) p.counters[w0] = 0u;
+          s_last = done == w1 - w0;
+          if (s_last) p.counters[w0] = 0u;
         }
         __syncthreads();
-        if (s_flag) {
+        if (s_last) {
+          // ---- the pieces of the head, in the order of the workers: the factors of all of them, then the sums, a float4
+          // column per thread; where there are fewer columns than threads, groups of threads take every n-th piece
           __threadfence();
-          merge_pieces(pl.vp, start, n_tiles, warp, kWarps);
+          const int pieces = (int)(w1 - w0 + 1);
+          auto piece = [&](int i) { return (const float*)partial_of(w0 + i, i == 0); };
+          float* f = reinterpret_cast<float*>(ring);         // [pieces][16]
+          float4* sums = reinterpret_cast<float4*>(ring + ((size_t)pieces * 64 + 127) / 128 * 128);
+          for (int h = warp; h < n_q; h += kWarps) {
+            float top = kNegBig, l = 0.f;
+            for (int i = lane; i < pieces; i += 32) {
+              const float m = __ldcg(piece(i) + p.rows * D + h);
+              f[i * 16 + h] = m;
+              top = fmaxf(top, m);
+            }
+#pragma unroll
+            for (int s = 16; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+            for (int i = lane; i < pieces; i += 32) {
+              const float by = ex2(f[i * 16 + h] - top);
+              f[i * 16 + h] = by;
+              l = fmaf(__ldcg(piece(i) + p.rows * (D + 1) + h), by, l);
+            }
+#pragma unroll
+            for (int s = 16; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+            if (lane == 0) { s_m[h] = top; s_l[h] = l; }
+          }
+          __syncthreads();
+          const int cols = n_q * (D / 4), groups = max(1, kThreads / cols);
+          for (int item = tid; item < groups * cols; item += kThreads) {
+            const int col = item % cols, h = col / (D / 4), d4 = col % (D / 4);
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int i = item / cols; i < pieces; i += groups) {
+              const float4 x = __ldcg(reinterpret_cast<const float4*>(piece(i) + h * D) + d4);
+              const float by = f[i * 16 + h];
+              o.x = fmaf(x.x, by, o.x);
+              o.y = fmaf(x.y, by, o.y);
+              o.z = fmaf(x.z, by, o.z);
+              o.w = fmaf(x.w, by, o.w);
+            }
+            sums[item] = o;
+          }
+          __syncthreads();
+          for (int col = tid; col < cols; col += kThreads) {
+            const int h = col / (D / 4), d4 = col % (D / 4);
+            float4 o = sums[col];
+            for (int i = 1; i < groups; ++i) {
+              const float4 x = sums[i * cols + col];
+              o.x += x.x;
+              o.y += x.y;
+              o.z += x.z;
+              o.w += x.w;
+            }
+            const long long qh = (long long)head * p.g + qi * p.rows + h;
+            store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, inverse(s_l[h]), p.bf16 != 0);
+            if (d4 == 0) W::write_stats(p, seq, qh, s_m[h], s_l[h]);
+          }
         }
       }
-      done_to += t1 - t0;
-      if (done_to >= end) break;
-      do {
-        start += tiles_of(pl.len);
-        enter(pl, pl.vp + 1, start);
-      } while (pl.len == 0);
-      __syncthreads();                                       // the rings are free again, and s_flag
+      if (cut || start + (uint32_t)pl.end >= end) return;
+      do ++vp; while (s_len[vp] == 0);                       // the stream goes on: there is one
+      __syncthreads();                                       // the rings, the factors and s_last are free again
     }
   }
 }
 
-template <int D, int kFmt, int kNt, int kWpw>
+template <int D, int kFmt, int kNt, bool kCta>
 cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_t st) {
-  using G = Geo<D, kFmt>;
-  auto* kernel = ssd_paged_decode_kernel<D, kFmt, kNt, kWpw>;
+  using G = Geo<D, kFmt, kNt>;
+  auto* kernel = ssd_paged_decode_kernel<D, kFmt, kNt, kCta>;
   // once per device; host threads that meet here make the same idempotent call
   static std::atomic<bool> ready[64] = {};
   int dev = 0;
@@ -900,7 +1122,7 @@ cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(sms);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(G::kThreads);
   cfg.dynamicSmemBytes = G::kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -914,12 +1136,14 @@ cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_
 }
 
 template <int D, int kFmt>
-cudaError_t launch_paged_format(const PagedDecodeParams& p, int sms, cudaStream_t st) {
+cudaError_t launch_paged_format(const PagedDecodeParams& in, int sms, cudaStream_t st) {
+  PagedDecodeParams p = in;
+  p.whole_tiles = p.c.page_size % Geo<D, kFmt, 1>::kTile == 0;
   // Many heads: a warp per share, and no meeting of warps.  Few heads: a thread block per share, so that a head's
   // pieces to be merged through memory are at most one per thread block.
-  const bool many = (long long)p.c.n_seqs * p.c.H * p.qt >= 2ll * sms;
-  if (p.rows <= 8) return many ? launch_paged_kernel<D, kFmt, 1, 1>(p, sms, st) : launch_paged_kernel<D, kFmt, 1, kWarps>(p, sms, st);
-  return many ? launch_paged_kernel<D, kFmt, 2, 1>(p, sms, st) : launch_paged_kernel<D, kFmt, 2, kWarps>(p, sms, st);
+  const bool many = (long long)p.c.n_seqs * p.c.H * p.qt > kPagedFewHeads;
+  if (p.rows <= 8) return many ? launch_paged_kernel<D, kFmt, 1, false>(p, sms, st) : launch_paged_kernel<D, kFmt, 1, true>(p, sms, st);
+  return many ? launch_paged_kernel<D, kFmt, 2, false>(p, sms, st) : launch_paged_kernel<D, kFmt, 2, true>(p, sms, st);
 }
 
 }  // namespace paged
