@@ -38,11 +38,11 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
     int a = 0, b = c.n_seqs;
     while (a < b) {
       const int m = (a + b) >> 1;
-      if (__ldg(p.cu + m) <= token) a = m + 1; else b = m;
+      if (p.cu[m] <= token) a = m + 1; else b = m;
     }
     seq = a - 1;
     if (seq < 0) return;
-    ago = __ldg(p.cu + seq + 1) - token;            // 1 for a sequence's newest token
+    ago = p.cu[seq + 1] - token;            // 1 for a sequence's newest token
     if (ago <= 0) return;
   }
   uint4 raw[kIters];
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
   for (int it = 0; it < kIters; ++it) {
     const int r = it * kRows + lane / kL, head = head0 + (r >> 1);
     raw[it] = make_uint4(0u, 0u, 0u, 0u);
-    if (head < c.H) raw[it] = __ldg(reinterpret_cast<const uint4*>((r & 1 ? p.v_new : p.k_new) + token * p.token_b + head * p.head_b) + lane % kL);
+    if (head < c.H) raw[it] = reinterpret_cast<const uint4*>((r & 1 ? p.v_new : p.k_new) + token * p.token_b + head * p.head_b)[lane % kL];
   }
 #pragma unroll
   for (int it = 0; it < kIters; ++it) {
@@ -85,28 +85,124 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
   }
 }
 
-// ----------------------------------------------------------------------------- weights
-// scores += sum over the query heads of a key head of 2^(logit - m) / l, from the logits and (m, l) that the attention
-// launch before it left: 4 bytes read per query head and slot, against 2 row bytes of K and V there.
+// ----------------------------------------------------------------------------- joining pieces, and the weights
+// After an attention launch that shared tiles out by warps: the pieces of every head that a share's border has cut are
+// joined, in the order of the workers: by a warp per query head, or by all eight of a thread block where there are many.
+// Where the weights are wanted, further thread blocks add them to the scores meanwhile:
+//   scores += sum over the query heads of a key head of 2^(logit - m) / l,
+// from the logits that the attention launch left (4 bytes per query head and slot, against 2 row bytes of K and V there),
+// with (m, l) from the pieces.
+constexpr int kJoinWarps = kThreads / 32;
+constexpr int kAlone = 16;                          // pieces up to which one warp joins them
 constexpr int kWeightSlots = 4 * kThreads;          // slots of a thread block
 
-__global__ void __launch_bounds__(kThreads) ssd_paged_weights_kernel(const __grid_constant__ PagedDecodeParams p, int blocks_per_pair) {
+__device__ __forceinline__ const float* piece_of(const PagedDecodeParams& p, int floats, int w0, int i) {
+  return p.partial + ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * floats;
+}
+
+template <int D>
+__device__ void join_heads(const PagedDecodeParams& p, int units) {
+  __shared__ int2 s_pc[kJoinWarps];
+  __shared__ float4 s_o[kJoinWarps][D / 4];
+  __shared__ float s_m[kJoinWarps], s_l[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int floats = paged_part_floats(p.rows, D);
+  const int unit0 = blockIdx.x * kJoinWarps;
+  auto of = [&](int unit, int& h, long long& at, char*& out) {        // a query head: its row in a state, and its place
+    const int vp = unit / p.rows;
+    h = unit - vp * p.rows;
+    const int pair = (int)p.by_qt.div((uint32_t)vp), qi = vp - pair * p.qt;
+    const int seq = (int)p.by_heads.div((uint32_t)pair), head = pair - seq * p.c.H;
+    const long long qh = (long long)head * p.g + qi * p.rows + h;
+    at = (long long)seq * p.c.H * p.g + qh;
+    out = p.out + seq * p.o_seq + qh * p.o_head;
+    return qi * p.rows + h < p.g;
+  };
+  auto finish = [&](int unit, const float4& o, float m, float l) {
+    int h;
+    long long at;
+    char* out;
+    of(unit, h, at, out);
+    if (lane < D / 4) paged_store4(out + 8 * lane, o, paged_inverse(l), p.bf16 != 0);
+    if (lane == 0) paged_stats(p, at, m, l);
+  };
+  int h = 0;
+  int2 pc = make_int2(0, 0);
+  if (unit0 + warp < units) {
+    long long at;
+    char* out;
+    if (of(unit0 + warp, h, at, out)) pc = __ldcg(p.pieces + (unit0 + warp) / p.rows);
+  }
+  if (lane == 0) s_pc[warp] = pc;
+  float4 o;
+  float m, l;
+  if (pc.y > 1 && pc.y <= kAlone) {
+    paged_merge<D>(p, lane, h, pc.y, [&](int i) { return piece_of(p, floats, pc.x, i); }, o, m, l);
+    finish(unit0 + warp, o, m, l);
+  }
+  __syncthreads();
+  for (int u = 0; u < kJoinWarps; ++u) {
+    const int2 q = s_pc[u];
+    if (q.y <= kAlone) continue;
+    const int hu = (unit0 + u) % p.rows;
+    const int n = (q.y - warp + kJoinWarps - 1) / kJoinWarps;
+    paged_merge<D>(p, lane, hu, n, [&](int i) { return piece_of(p, floats, q.x, i * kJoinWarps + warp); }, o, m, l);
+    if (lane < D / 4) s_o[warp][lane] = o;
+    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+    __syncthreads();
+    if (warp == u) {
+      float top = s_m[0], sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w]);
+      float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = ex2(s_m[w] - top);
+        sum = fmaf(s_l[w], f, sum);
+        const float4 x = s_o[w][lane % (D / 4)];
+        r.x = fmaf(x.x, f, r.x);
+        r.y = fmaf(x.y, f, r.y);
+        r.z = fmaf(x.z, f, r.z);
+        r.w = fmaf(x.w, f, r.w);
+      }
+      finish(unit0 + u, r, top, sum);
+    }
+    __syncthreads();
+  }
+}
+
+// The scores of kWeightSlots slots of one (sequence, key head).  head_dim: that of the states in p.partial.
+__device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_per_pair, int head_dim, bool joined) {
   __shared__ float2 s_ml[128];
   const PagedView& c = p.c;
-  const int pair = blockIdx.x / blocks_per_pair, part = blockIdx.x - pair * blocks_per_pair;
-  const int seq = pair / c.H, head = pair - seq * c.H;
-  pdl_wait_predecessor();
-  pdl_allow_successor();
+  const int pair = block / blocks_per_pair, part = block - pair * blocks_per_pair;
+  const int seq = (int)p.by_heads.div((uint32_t)pair), head = pair - seq * c.H;
   const int len = paged_length(c, seq, head);
   const int first = part * kWeightSlots;
   if (first >= len) return;
   float* scores = paged_scores(c, seq, head);
+  const int floats = paged_part_floats(p.rows, head_dim);
   float w[4] = {0.f, 0.f, 0.f, 0.f};
   for (int h0 = 0; h0 < p.g; h0 += 128) {
     const int n = min(128, p.g - h0);
     __syncthreads();
     for (int h = threadIdx.x; h < n; h += kThreads) {
-      float2 x = __ldg(p.ml + (size_t)pair * p.g + h0 + h);
+      const int qi = (h0 + h) / p.rows, row = h0 + h - qi * p.rows;
+      const int2 pc = joined ? __ldcg(p.pieces + pair * p.qt + qi) : make_int2(0, 1);
+      float2 x;
+      if (pc.y == 1) {
+        x = __ldcg(p.ml + (size_t)pair * p.g + h0 + h);
+      } else {
+        x = make_float2(kNegBig, 0.f);
+#pragma unroll 8
+        for (int i = 0; i < pc.y; ++i) x.x = fmaxf(x.x, __ldcg(piece_of(p, floats, pc.x, i) + p.rows * head_dim + row));
+#pragma unroll 8
+        for (int i = 0; i < pc.y; ++i) {
+          const float* s = piece_of(p, floats, pc.x, i) + p.rows * head_dim + row;
+          x.y = fmaf(__ldcg(s + p.rows), ex2(__ldcg(s) - x.x), x.y);
+        }
+        x.x -= kPagedShift;
+      }
       x.y = x.y == 0.f ? 0.f : 1.f / x.y;
       s_ml[h] = x;
     }
@@ -118,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_weights_kernel(const __gri
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int s = i * kThreads + threadIdx.x;
-        if (first + s < len) w[i] += ex2(__ldg(logits + h * p.logit_row + s) - ml.x) * ml.y;
+        if (first + s < len) w[i] += ex2(__ldcg(logits + h * p.logit_row + s) - ml.x) * ml.y;
       }
     }
   }
@@ -130,6 +226,19 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_weights_kernel(const __gri
     else if (p.k_new && slot == len - 1) scores[slot] = w[i];        // the token being appended has had none before
     else scores[slot] += w[i];
   }
+}
+
+struct JoinParams {
+  PagedDecodeParams d;
+  int join_blocks, units, blocks_per_pair;   // the thread blocks after the first join_blocks add weights
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) ssd_paged_join_kernel(const __grid_constant__ JoinParams p) {
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units);
+  else add_weights(p.d, blockIdx.x - p.join_blocks, p.blocks_per_pair, D, p.join_blocks > 0);
 }
 
 // ----------------------------------------------------------------------------- eviction: which tokens stay
@@ -302,7 +411,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_c
   const bool scales = a.ks != nullptr && (chunk == 0 || chunk == kCpr);
   pdl_wait_predecessor();
   pdl_allow_successor();
-  const int count = __ldg(p.counts + pair);
+  const int count = __ldcg(p.counts + pair);
   const int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
   if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) b.lens[seq * b.n_seq + head * b.n_head] = count;
   const int32_t* ta = paged_table(a, seq, head);
@@ -318,7 +427,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_c
       const int j = j0 + (u * (kThreads / 32) + warp) * kRpi + lane / kL;
       page[u] = -1;
       if (j < count) {
-        const int s = __ldg(kept + j);
+        const int s = __ldcg(kept + j);
         if (!(kInPlace && s == j) && s >= 0 && s < a.cap) {
           int r;
           const int g = paged_lookup(a, ta, s, r);
@@ -426,10 +535,10 @@ int sm_count(int* sms) {
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
-// [counters | partial states | (max, sum) | logits].  The counters, the only part that has to be zero between calls, lie
+// [counters | partial states | pieces of a head | (max, sum) | logits].  The counters, the only part that has to be zero between calls, lie
 // at the same place whatever the call's sizes: caches of any shapes can share a workspace.
 struct Workspace {
-  size_t partial, ml, logits, bytes;
+  size_t partial, pieces, ml, logits, bytes;
 };
 
 Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate, int sms) {
@@ -437,7 +546,8 @@ Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate,
   const size_t heads = (size_t)v.n_seqs * v.H * g;
   Workspace w;
   w.partial = align_up(paged_max_workers(sms) * 4);
-  w.ml = align_up(w.partial + paged_max_workers(sms) * 2 * paged_part_floats(rows, head_dim) * 4);
+  w.pieces = align_up(w.partial + paged_max_workers(sms) * 2 * paged_part_floats(rows, head_dim) * 4);
+  w.ml = align_up(w.pieces + (size_t)v.n_seqs * v.H * ((g + rows - 1) / rows) * 8);
   w.logits = align_up(w.ml + (accumulate ? heads * 8 : 0));
   w.bytes = w.logits + (accumulate ? heads * (size_t)v.cap * 4 : 0);
   return w;
@@ -489,6 +599,7 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   char* ws = static_cast<char*>(a->workspace);
   p.counters = reinterpret_cast<uint32_t*>(ws);
   p.partial = reinterpret_cast<float*>(ws + w.partial);
+  p.pieces = reinterpret_cast<int2*>(ws + w.pieces);
   if (a->accumulate) {
     p.ml = reinterpret_cast<float2*>(ws + w.ml);
     p.logits = reinterpret_cast<float*>(ws + w.logits);
@@ -499,30 +610,21 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   p.bf16 = a->q_dtype == SSD_PAGED_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = kv->dtype == SSD_PAGED_E4M3 ? launch_paged_decode_8(p, kv->head_dim, sms, st) : launch_paged_decode_16(p, kv->head_dim, sms, st);
-  if (e == cudaSuccess && a->accumulate) e = launch_paged_weights(p, st);
+  const bool many = paged_many(p, sms);
+  if (e == cudaSuccess && (many || a->accumulate)) {
+    JoinParams j = {};
+    j.d = p;
+    j.units = p.c.n_seqs * p.c.H * p.qt * p.rows;
+    j.join_blocks = many ? (j.units + kJoinWarps - 1) / kJoinWarps : 0;
+    j.blocks_per_pair = (p.c.cap + kWeightSlots - 1) / kWeightSlots;
+    const int blocks = j.join_blocks + (a->accumulate ? p.c.n_seqs * p.c.H * j.blocks_per_pair : 0);
+    e = launch<JoinParams>(kv->head_dim == 128 ? ssd_paged_join_kernel<128> : ssd_paged_join_kernel<64>, dim3((unsigned)blocks), kThreads, 0, st, j);
+  }
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;
 }
 
 }  // namespace
-
-cudaError_t launch_paged_weights(const PagedDecodeParams& p, cudaStream_t st) {
-  const int per = (p.c.cap + kWeightSlots - 1) / kWeightSlots;
-  const long long blocks = (long long)p.c.n_seqs * p.c.H * per;
-  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, ssd_paged_weights_kernel, p, per);
-  count_launch();
-  return e;
-}
 
 }  // namespace ssd
 

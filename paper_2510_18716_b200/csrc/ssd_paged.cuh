@@ -11,6 +11,10 @@
 
 namespace ssd {
 
+// The paged kernels are launched as programmatic dependents of whatever is before them, and may start while that still
+// runs.  They read nothing before pdl_wait_predecessor(), and what an earlier kernel may have written never through the
+// non-coherent path (__ldg): ordinary loads, or __ldcg for what another SM's thread blocks left for this launch.
+
 // Bits of the cache's device status word: what a kernel met in device data and left out.
 constexpr uint32_t kPagedBadPage = 1u;     // a page number outside the pool: the slot counts as masked, is not written
 constexpr uint32_t kPagedBadLength = 2u;   // a length outside [0, capacity]: it is cut to that range
@@ -60,7 +64,7 @@ __device__ __forceinline__ void paged_split(const PagedView& c, int slot, int& i
 __device__ __forceinline__ int paged_lookup(const PagedView& c, const int32_t* table, int slot, int& row) {
   int index;
   paged_split(c, slot, index, row);
-  const int page = __ldg(table + index);
+  const int page = table[index];
   if ((uint32_t)page < (uint32_t)c.n_pages) return page;
   paged_flag(c, kPagedBadPage);
   return -1;
@@ -142,6 +146,7 @@ struct PagedDecodeParams {
   float2* ml;               // weights wanted: [n_seqs * H * g] (max, sum)
   long long logit_row;
   uint32_t* counters;       // [workers], zero between launches
+  int2* pieces;             // [n_seqs * H * qt]: the first worker that has a piece of the head, and how many have
   float* partial;           // [workers][2][paged_part_floats(rows, D)]
   float scale_log2;
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together
@@ -161,9 +166,80 @@ __host__ __device__
 #endif
 inline int paged_part_floats(int rows, int head_dim) { return (rows * (head_dim + 2) + 3) / 4 * 4; }
 
+// Whether a launch shares out tiles by warps (and leaves pieces to ssd_paged_join_kernel), or whole pieces by thread blocks,
+// which loses up to a third of them where there are as many heads as a quarter of the SMs.
+inline bool paged_many(const PagedDecodeParams& p, int sms) { return (long long)p.c.n_seqs * p.c.H * p.qt > sms / 4; }
+
+#if defined(__CUDACC__)
+constexpr float kPagedShift = 14.f;          // the weights are held 2^14 times too large, and l with them
+constexpr float kPagedNegInf = -__builtin_huge_valf();
+
+__device__ __forceinline__ float paged_inverse(float l) { return l > 0.f ? 1.f / l : l; }   // no row at all: zeros (a NaN stays one)
+// A query head's final (m, l), m in base 2, at its place in [n_seqs, H * g]
+__device__ __forceinline__ void paged_stats(const PagedDecodeParams& p, long long at, float m, float l) {
+  if (p.lse) p.lse[at] = l == 0.f ? kPagedNegInf : (m + log2f(l) - kPagedShift) * 0.69314718055994530942f;
+  if (p.ml) p.ml[at] = make_float2(m - kPagedShift, l);
+}
+
+// One query head's n pieces of one head, merged by a warp, in order: lane d4 < D / 4 ends with four sums (D == 64: lanes
+// 16 .. 31 hold the pieces of odd number until the end).  piece(i) is the memory of a state, read past L1.
+template <int D, class F>
+__device__ __forceinline__ void paged_merge(const PagedDecodeParams& p, int lane, int h, int n, F piece, float4& o, float& m, float& l) {
+  constexpr int kGroups = 128 / D;
+  m = kNegBig;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, __ldcg(piece(i) + p.rows * D + h));
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+  l = 0.f;
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float f = 0.f;
+    if (i0 + lane < n) {
+      f = ex2(__ldcg(piece(i0 + lane) + p.rows * D + h) - m);
+      l = fmaf(__ldcg(piece(i0 + lane) + p.rows * (D + 1) + h), f, l);
+    }
+    const int top = min(32, n - i0);
+#pragma unroll 8
+    for (int i = 0; i < top; i += kGroups) {
+      const int mine = i + lane / (D / 4);
+      const float by = __shfl_sync(0xffffffffu, f, mine);
+      if (mine < top) {
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(piece(i0 + mine) + h * D) + lane % (D / 4));
+        o.x = fmaf(x.x, by, o.x);
+        o.y = fmaf(x.y, by, o.y);
+        o.z = fmaf(x.z, by, o.z);
+        o.w = fmaf(x.w, by, o.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+  if constexpr (kGroups == 2) {
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
+    o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
+    o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+  }
+}
+
+__device__ __forceinline__ void paged_store4(char* to, const float4& x, float by, bool bf16) {
+  uint2 w;
+  if (bf16) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x * by, x.y * by), b = __floats2bfloat162_rn(x.z * by, x.w * by);
+    memcpy(&w.x, &a, 4);
+    memcpy(&w.y, &b, 4);
+  } else {
+    const __half2 a = __floats2half2_rn(x.x * by, x.y * by), b = __floats2half2_rn(x.z * by, x.w * by);
+    memcpy(&w.x, &a, 4);
+    memcpy(&w.y, &b, 4);
+  }
+  *reinterpret_cast<uint2*>(to) = w;
+}
+#endif
+
 cudaError_t launch_paged_decode_16(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st);
 cudaError_t launch_paged_decode_8(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st);
-cudaError_t launch_paged_weights(const PagedDecodeParams& p, cudaStream_t st);
+
 size_t paged_max_workers(int sms);
 
 }  // namespace ssd

@@ -4,13 +4,16 @@
 //   x_hj = scale q_h . k_j,   m_h = max_j x_hj,   l_h = sum_j e^(x_hj - m_h),   o_h = sum_j e^(x_hj - m_h) v_j / l_h.
 // One pass over K and V with a running maximum and sum; every byte of them is read once per group of <= 16 query heads.
 //
-// Work: the slots of a key head are cut into tiles of 8 KB (4 KB of K, 4 KB of V).  The tiles of all (sequence, head,
-// group) are one stream, cut into equal shares, one per worker, from the lengths that the launch finds on the device.
-// A worker is one warp, or all warps of a thread block (kCta), which take a head's tiles in turn and
-// merge their states in shared memory.  Heads cut by a share's border leave (O, m, l) of each piece in global memory;
-// whoever completes the last piece (a counter, kept under the worker that has the head's first piece: a worker has at
-// most one head that starts in its share and is cut at its end) merges them in the order of the workers: the result does not
-// depend on who that is, and nobody waits for another.
+// Work: the slots of a key head are cut into tiles of 8 KB (4 KB of K, 4 KB of V).
+// Many heads (!kCta): the tiles of all (sequence, head, group) are one stream, cut into equal shares, one per warp of the
+// launch, from the lengths that the launch finds on the device.  A warp runs through the heads of its share without ever
+// meeting another; of a head that a share's border cuts it leaves a piece, (O, m, l), and a second launch joins the pieces
+// (ssd_paged_join_kernel).  Joining them here, by whoever completes the last one, was 48 us slower at 16 x 8 heads of up to
+// 32768 slots: one warp merged 15 pieces of 8 query heads while the others were done.
+// Few heads (kCta): a piece is a run of tiles of one head for a whole thread block, whose warps take them in turn and merge
+// in shared memory.  The pieces of a head meet in global memory, where the thread block that completes the last one
+// (a counter, kept under the worker of the head's first piece) joins them: one launch, for the calls whose latency counts.
+// Both ways pieces are joined in the order of the workers: the result does not depend on who is first, and nobody waits.
 //
 // A warp keeps kStages tiles of its own in shared memory and fills them with 16-byte asynchronous copies, row by row
 // (pages may have any size and strides), zeros in the place of rows that do not exist: a NaN behind the last row, or
@@ -20,7 +23,7 @@
 // fill the 16 rows of an m16n8k16 product and the query heads its 8 columns (kNt = 2: 16 heads).  The work is bound by
 // the bytes of K and V (per 8 KB tile: 24 products and 16 ldmatrix for 8 heads, a fraction of the 8 KB's time on HBM).
 // The weights are rounded to 16 bits for the second product as a sum of two 16-bit terms, which keeps 16 (bf16) or 22
-// (fp16) bits of them; all sums are in 32 bits.  The weights are held 2^14 times too large (kShift) so that the small
+// (fp16) bits of them; all sums are in 32 bits.  The weights are held 2^14 times too large (kPagedShift) so that the small
 // ones of a long row stay normal numbers in fp16; the factor is in l too and cancels.
 // 8-bit rows are widened to fp16, which holds every code exactly; q is brought into fp16's range by a power of two per
 // head, the K scale multiplies the logit, and the V scale's power of two 2^e is added to it: the running maximum is that
@@ -34,13 +37,7 @@
 namespace ssd {
 namespace paged {
 
-constexpr float kShift = 14.f;
-constexpr float kNegInf = -__builtin_huge_valf();
 
-#ifndef SSD_PAGED_FEW
-#define SSD_PAGED_FEW 256
-#endif
-constexpr int kPagedFewHeads = SSD_PAGED_FEW;   // not above the threads of a thread block
 #ifndef SSD_PAGED_WARPS1
 #define SSD_PAGED_WARPS1 12
 #define SSD_PAGED_STAGES1 2
@@ -132,8 +129,6 @@ __device__ __forceinline__ void store16(char* to, float x, bool bf16) {
   else
     *reinterpret_cast<__half*>(to) = __float2half_rn(x);
 }
-
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }   // no row at all: zeros (a NaN stays one)
 
 // A place in the stream of tiles.
 struct Place {
@@ -246,7 +241,7 @@ struct Worker {
     if (p.whole_tiles) {
       int index;
       paged_split(p.c, at.t * G::kTile, index, r.row[0]);
-      r.page[0] = __ldg(table + index);
+      r.page[0] = table[index];
       return;
     }
 #pragma unroll
@@ -258,7 +253,7 @@ struct Worker {
       if (local < G::kTile && slot < at.len) {
         int index;
         paged_split(p.c, slot, index, r.row[i]);
-        r.page[i] = __ldg(table + index);
+        r.page[i] = table[index];
       }
     }
   }
@@ -378,7 +373,7 @@ struct Worker {
     const int part = lane & 15;
     const bool mine = part < kL;
     const char* from = (lane < 16 ? p.k_new : p.v_new) + seq * p.new_seq + head * p.new_head;
-    const uint4 raw = mine ? __ldg(reinterpret_cast<const uint4*>(from) + part) : make_uint4(0u, 0u, 0u, 0u);
+    const uint4 raw = mine ? reinterpret_cast<const uint4*>(from)[part] : make_uint4(0u, 0u, 0u, 0u);
     const bool ok = (uint32_t)page < (uint32_t)c.n_pages;
     const bool store = ok && qi == 0;
     const long long off = ok ? page * c.page_b + head * c.head_b + row * c.slot_b : 0;
@@ -458,7 +453,7 @@ struct Worker {
           for (int e = 0; e < 2; ++e) {
             float& x = s[sb][nt][2 * hf + e];
             x += s2[sb][nt][2 * hf + e];
-            x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kNegInf;
+            x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kPagedNegInf;
           }
       }
     }
@@ -483,7 +478,7 @@ struct Worker {
     }
     float top[kNt][2];
 #pragma unroll
-    for (int nt = 0; nt < kNt; ++nt) top[nt][0] = top[nt][1] = kNegInf;
+    for (int nt = 0; nt < kNt; ++nt) top[nt][0] = top[nt][1] = kPagedNegInf;
 #pragma unroll
     for (int sb = 0; sb < kSub; ++sb)
 #pragma unroll
@@ -541,8 +536,8 @@ struct Worker {
       for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          float w0 = ex2(s[sb][nt][2 * hf] - (m[nt][0] - kShift));
-          float w1 = ex2(s[sb][nt][2 * hf + 1] - (m[nt][1] - kShift));
+          float w0 = ex2(s[sb][nt][2 * hf] - (m[nt][0] - kPagedShift));
+          float w1 = ex2(s[sb][nt][2 * hf + 1] - (m[nt][1] - kPagedShift));
           if constexpr (kFmt == kPagedE4m3) {
             l[nt][0] = fmaf(w0, vinv[sb][hf], l[nt][0]);
             l[nt][1] = fmaf(w1, vinv[sb][hf], l[nt][1]);
@@ -634,78 +629,18 @@ struct Worker {
         if (h < n_q) {
           const long long qh = (long long)head * p.g + qi * p.rows + h;
           char* to = p.out + seq * p.o_seq + qh * p.o_head;
-          const float by = inverse(l[nt][e]);
+          const float by = paged_inverse(l[nt][e]);
 #pragma unroll
           for (int mt = 0; mt < kKs; ++mt) {
             store16(to + 2 * dim_of(mt, 0), o[nt][mt][e] * by, p.bf16 != 0);
             store16(to + 2 * dim_of(mt, 1), o[nt][mt][2 + e] * by, p.bf16 != 0);
           }
-          if ((lane >> 2) == 0) write_stats(p, seq, qh, m[nt][e], l[nt][e]);
+          if ((lane >> 2) == 0) paged_stats(p, (long long)seq * p.c.H * p.g + qh, m[nt][e], l[nt][e]);
         }
       }
   }
-
-  static __device__ __forceinline__ void write_stats(const PagedDecodeParams& p, int seq, long long qh, float m, float l) {
-    const long long at = (long long)seq * p.c.H * p.g + qh;
-    if (p.lse) p.lse[at] = l == 0.f ? kNegInf : (m + log2f(l) - kShift) * 0.69314718055994530942f;
-    if (p.ml) p.ml[at] = make_float2(m - kShift, l);
-  }
 };
 
-// One query head's n pieces of one head, merged by a warp, in order: lane d4 < D / 4 ends with four sums (D == 64: lanes
-// 16 .. 31 hold the pieces of odd number until the end).  piece(i) is the memory of a state, read past L1.
-template <int D, class F>
-__device__ __forceinline__ void merge_head(const PagedDecodeParams& p, int lane, int h, int n, F piece, float4& o, float& m, float& l) {
-  constexpr int kGroups = 128 / D;
-  m = kNegBig;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, __ldcg(piece(i) + p.rows * D + h));
-#pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-  l = 0.f;
-  o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    float f = 0.f;
-    if (i0 + lane < n) {
-      f = ex2(__ldcg(piece(i0 + lane) + p.rows * D + h) - m);
-      l = fmaf(__ldcg(piece(i0 + lane) + p.rows * (D + 1) + h), f, l);
-    }
-    const int top = min(32, n - i0);
-#pragma unroll 4
-    for (int i = 0; i < top; i += kGroups) {
-      const int mine = i + lane / (D / 4);
-      const float by = __shfl_sync(0xffffffffu, f, mine);
-      if (mine < top) {
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(piece(i0 + mine) + h * D) + lane % (D / 4));
-        o.x = fmaf(x.x, by, o.x);
-        o.y = fmaf(x.y, by, o.y);
-        o.z = fmaf(x.z, by, o.z);
-        o.w = fmaf(x.w, by, o.w);
-      }
-    }
-  }
-#pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-  if constexpr (kGroups == 2) {
-    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
-    o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
-    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
-    o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
-  }
-}
-
-__device__ __forceinline__ void store4(char* to, const float4& x, float by, bool bf16) {
-  uint2 w;
-  if (bf16) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x * by, x.y * by), b = __floats2bfloat162_rn(x.z * by, x.w * by);
-    memcpy(&w.x, &a, 4);
-    memcpy(&w.y, &b, 4);
-  } else {
-    const __half2 a = __floats2half2_rn(x.x * by, x.y * by), b = __floats2half2_rn(x.z * by, x.w * by);
-    memcpy(&w.x, &a, 4);
-    memcpy(&w.y, &b, 4);
-  }
-  *reinterpret_cast<uint2*>(to) = w;
-}
 template <int kThreads>
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uint32_t& total) {   // exclusive sum
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -761,7 +696,7 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     for (int h = qi * p.rows; h < min(p.g, (qi + 1) * p.rows); ++h) {
       const long long qh = (long long)head * p.g + h;
       for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + seq * p.o_seq + qh * p.o_head + 2 * d) = make_uint4(0u, 0u, 0u, 0u);
-      W::write_stats(p, seq, qh, kNegBig, 0.f);
+      paged_stats(p, (long long)seq * c.H * p.g + qh, kNegBig, 0.f);
     }
   };
   const int part_floats = paged_part_floats(p.rows, D);
@@ -779,7 +714,10 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     for (int i = lo; i < hi; ++i) {
       const int len = length_of(i);
       sum += tiles_of(len);
-      if (len == 0 && (uint32_t)i % gridDim.x == blockIdx.x) zeros(i);
+      if (len == 0 && (uint32_t)i % gridDim.x == blockIdx.x) {
+        zeros(i);
+        p.pieces[i] = make_int2(0, 0);
+      }
     }
     s_pref[tid] = block_scan<kThreads>(sum, s_warp, total);
     __syncthreads();
@@ -867,29 +805,9 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       if (now.t + 1 == now.end) {
         w.close();
         const uint32_t w0 = start_n / share, w1 = (start_n + tiles_of(now.len) - 1) / share;
-        const int n_q = min(p.g - qi * p.rows, p.rows);
-        if (w0 == w1) {
-          w.write_out(seq, head, qi);
-        } else {
-          w.write_state(partial_of(worker, worker == w0), D, n_q);
-          __threadfence();
-          __syncwarp();
-          uint32_t done = 0u;
-          if (lane == 0) done = atomicAdd(p.counters + w0, 1u);
-          done = __shfl_sync(0xffffffffu, done, 0);
-          if (done == w1 - w0) {
-            __threadfence();
-            if (lane == 0) p.counters[w0] = 0u;
-            for (int h = 0; h < n_q; ++h) {
-              float4 o;
-              float m, l;
-              merge_head<D>(p, lane, h, (int)(w1 - w0 + 1), [&](int k) { return (const float*)partial_of(w0 + k, k == 0); }, o, m, l);
-              const long long qh = (long long)head * p.g + qi * p.rows + h;
-              if (lane < D / 4) store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * lane, o, inverse(l), p.bf16 != 0);
-              if (lane == 0) W::write_stats(p, seq, qh, m, l);
-            }
-          }
-        }
+        if (lane == 0 && worker == w0) p.pieces[now.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
+        if (w0 == w1) w.write_out(seq, head, qi);
+        else w.write_state(partial_of(worker, worker == w0), D, min(p.g - qi * p.rows, p.rows));
       }
       if (i < n + kStages - 2 && advance(now, start_n)) {
         name(now.vp, seq, head, qi);
@@ -914,52 +832,27 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     const uint32_t n_held = (uint32_t)__syncthreads_count(len > 0);
     if (total == 0u) return;
     const uint32_t workers = gridDim.x, worker = blockIdx.x;
-    // Equal shares of the stream, which leave a worker with pieces of two heads, one after the other; or, where that
-    // costs little, whole pieces of one head each: pieces of `cut` tiles, of which there are at most `workers`.  A second
-    // piece costs a worker some 3 us (its first loads, and merging twice), the time of 16 tiles.
-    uint32_t share = max((total + workers - 1) / workers, (uint32_t)kWarps);
-    uint32_t cut = 0u;
-    if (n_held < workers) {
-      cut = max((total + workers - n_held - 1) / (workers - n_held), (uint32_t)kWarps);
-      if (cut > share + 16u) cut = 0u;
-    }
-    uint32_t first, end;
-    if (cut) {
-      const uint32_t pieces = (tiles + cut - 1) / cut;
-      uint32_t all;
-      before = block_scan<kThreads>(pieces, s_warp, all);
-      if (worker >= all) return;
-      if (before <= worker && worker < before + pieces) s_vp = tid;
-      first = end = 0u;
-    } else {
-      first = worker * share;
-      end = min(total, first + share);
-      if (first >= end) return;
-      if (before <= first && first < before + tiles) s_vp = tid;
-    }
+    // pieces of `cut` tiles of one head each, of which there are at most `workers`: sum ceil(t / cut) <= sum t / cut + heads
+    const uint32_t cut = max((total + workers - n_held - 1) / (workers - n_held), (uint32_t)kWarps);
+    const uint32_t pieces = (tiles + cut - 1) / cut;
+    uint32_t all;
+    before = block_scan<kThreads>(pieces, s_warp, all);
+    if (worker >= all) return;
+    if (before <= worker && worker < before + pieces) s_vp = tid;
     s_pref[tid] = before;
     __syncthreads();
-    for (int vp = s_vp;;) {
+    {
+      const int vp = s_vp;
       int seq, head, qi;
       name(vp, seq, head, qi);
       const int n_q = min(p.g - qi * p.rows, p.rows);
       Place pl;
       pl.vp = vp;
       pl.len = s_len[vp];
-      const uint32_t n_tiles = tiles_of(pl.len), start = s_pref[vp];
-      uint32_t w0, w1;                                       // the workers that share this head
-      int t0;
-      if (cut) {
-        w0 = start;
-        w1 = start + (n_tiles - 1) / cut;
-        t0 = (int)((worker - w0) * cut);
-        pl.end = (int)min(n_tiles, t0 + cut);
-      } else {
-        w0 = start / share;
-        w1 = (start + n_tiles - 1) / share;
-        t0 = first > start ? (int)(first - start) : 0;
-        pl.end = (int)min(n_tiles, end - start);
-      }
+      const uint32_t n_tiles = tiles_of(pl.len);
+      const uint32_t w0 = s_pref[vp], w1 = w0 + (n_tiles - 1) / cut;         // the workers that share this head
+      const int t0 = (int)((worker - w0) * cut);
+      pl.end = (int)min(n_tiles, t0 + cut);
       Place now = pl;
       pl.t = now.t = t0 + warp;
       const int n = pl.end > pl.t ? (pl.end - pl.t + kWarps - 1) / kWarps : 0;
@@ -1021,8 +914,8 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
           }
         if (whole) {
           const long long qh = (long long)head * p.g + qi * p.rows + h;
-          store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, inverse(s_l[h]), p.bf16 != 0);
-          if (d4 == 0) W::write_stats(p, seq, qh, s_m[h], s_l[h]);
+          paged_store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, paged_inverse(s_l[h]), p.bf16 != 0);
+          if (d4 == 0) paged_stats(p, (long long)seq * c.H * p.g + qh, s_m[h], s_l[h]);
         } else {
           __stcg(reinterpret_cast<float4*>(part + h * D) + d4, o);
           if (d4 == 0) {
@@ -1094,14 +987,11 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
               o.w += x.w;
             }
             const long long qh = (long long)head * p.g + qi * p.rows + h;
-            store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, inverse(s_l[h]), p.bf16 != 0);
-            if (d4 == 0) W::write_stats(p, seq, qh, s_m[h], s_l[h]);
+            paged_store4(p.out + seq * p.o_seq + qh * p.o_head + 8 * d4, o, paged_inverse(s_l[h]), p.bf16 != 0);
+            if (d4 == 0) paged_stats(p, (long long)seq * c.H * p.g + qh, s_m[h], s_l[h]);
           }
         }
       }
-      if (cut || start + (uint32_t)pl.end >= end) return;
-      do ++vp; while (s_len[vp] == 0);                       // the stream goes on: there is one
-      __syncthreads();                                       // the rings, the factors and s_last are free again
     }
   }
 }
@@ -1139,9 +1029,7 @@ template <int D, int kFmt>
 cudaError_t launch_paged_format(const PagedDecodeParams& in, int sms, cudaStream_t st) {
   PagedDecodeParams p = in;
   p.whole_tiles = p.c.page_size % Geo<D, kFmt, 1>::kTile == 0;
-  // Many heads: a warp per share, and no meeting of warps.  Few heads: a thread block per share, so that a head's
-  // pieces to be merged through memory are at most one per thread block.
-  const bool many = (long long)p.c.n_seqs * p.c.H * p.qt > kPagedFewHeads;
+  const bool many = paged_many(p, sms);
   if (p.rows <= 8) return many ? launch_paged_kernel<D, kFmt, 1, false>(p, sms, st) : launch_paged_kernel<D, kFmt, 1, true>(p, sms, st);
   return many ? launch_paged_kernel<D, kFmt, 2, false>(p, sms, st) : launch_paged_kernel<D, kFmt, 2, true>(p, sms, st);
 }
