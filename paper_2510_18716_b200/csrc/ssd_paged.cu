@@ -101,13 +101,14 @@ __device__ __forceinline__ const float* piece_of(const PagedDecodeParams& p, int
 }
 
 template <int D>
-__device__ void join_heads(const PagedDecodeParams& p, int units) {
+__device__ void join_heads(const PagedDecodeParams& p, int units, int join_blocks) {
   __shared__ int2 s_pc[kJoinWarps];
   __shared__ float4 s_o[kJoinWarps][D / 4];
   __shared__ float s_m[kJoinWarps], s_l[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int floats = paged_part_floats(p.rows, D);
-  const int unit0 = blockIdx.x * kJoinWarps;
+  // heads that are cut into many pieces tend to be neighbours: the units of a thread block lie far apart
+  auto unit_of = [&](int w) { return w * (int)join_blocks + (int)blockIdx.x; };
   auto of = [&](int unit, int& h, long long& at, char*& out) {        // a query head: its row in a state, and its place
     const int vp = unit / p.rows;
     h = unit - vp * p.rows;
@@ -128,23 +129,24 @@ __device__ void join_heads(const PagedDecodeParams& p, int units) {
   };
   int h = 0;
   int2 pc = make_int2(0, 0);
-  if (unit0 + warp < units) {
+  const int mine = unit_of(warp);
+  if (mine < units) {
     long long at;
     char* out;
-    if (of(unit0 + warp, h, at, out)) pc = __ldcg(p.pieces + (unit0 + warp) / p.rows);
+    if (of(mine, h, at, out)) pc = __ldcg(p.pieces + mine / p.rows);
   }
   if (lane == 0) s_pc[warp] = pc;
   float4 o;
   float m, l;
   if (pc.y > 1 && pc.y <= kAlone) {
     paged_merge<D>(p, lane, h, pc.y, [&](int i) { return piece_of(p, floats, pc.x, i); }, o, m, l);
-    finish(unit0 + warp, o, m, l);
+    finish(mine, o, m, l);
   }
   __syncthreads();
   for (int u = 0; u < kJoinWarps; ++u) {
     const int2 q = s_pc[u];
     if (q.y <= kAlone) continue;
-    const int hu = (unit0 + u) % p.rows;
+    const int hu = unit_of(u) % p.rows;
     const int n = (q.y - warp + kJoinWarps - 1) / kJoinWarps;
     paged_merge<D>(p, lane, hu, n, [&](int i) { return piece_of(p, floats, q.x, i * kJoinWarps + warp); }, o, m, l);
     if (lane < D / 4) s_o[warp][lane] = o;
@@ -165,66 +167,77 @@ __device__ void join_heads(const PagedDecodeParams& p, int units) {
         r.z = fmaf(x.z, f, r.z);
         r.w = fmaf(x.w, f, r.w);
       }
-      finish(unit0 + u, r, top, sum);
+      finish(unit_of(u), r, top, sum);
     }
     __syncthreads();
   }
 }
 
-// The scores of kWeightSlots slots of one (sequence, key head).  head_dim: that of the states in p.partial.
+// The scores of kWeightSlots slots of one (sequence, key head), four neighbours per thread, eight query heads at a time:
+// their logits are on the way while each warp works out one query head's (m, l).  head_dim: that of the states in p.partial.
 __device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_per_pair, int head_dim, bool joined) {
-  __shared__ float2 s_ml[128];
+  __shared__ float2 s_ml[8];
   const PagedView& c = p.c;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int pair = block / blocks_per_pair, part = block - pair * blocks_per_pair;
   const int seq = (int)p.by_heads.div((uint32_t)pair), head = pair - seq * c.H;
   const int len = paged_length(c, seq, head);
-  const int first = part * kWeightSlots;
-  if (first >= len) return;
+  const int slot0 = part * kWeightSlots + 4 * (int)threadIdx.x;
+  if (part * kWeightSlots >= len) return;
   float* scores = paged_scores(c, seq, head);
   const int floats = paged_part_floats(p.rows, head_dim);
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int h0 = 0; h0 < p.g; h0 += 128) {
-    const int n = min(128, p.g - h0);
-    __syncthreads();
-    for (int h = threadIdx.x; h < n; h += kThreads) {
-      const int qi = (h0 + h) / p.rows, row = h0 + h - qi * p.rows;
-      const int2 pc = joined ? __ldcg(p.pieces + pair * p.qt + qi) : make_int2(0, 1);
-      float2 x;
-      if (pc.y == 1) {
-        x = __ldcg(p.ml + (size_t)pair * p.g + h0 + h);
-      } else {
-        x = make_float2(kNegBig, 0.f);
-#pragma unroll 8
-        for (int i = 0; i < pc.y; ++i) x.x = fmaxf(x.x, __ldcg(piece_of(p, floats, pc.x, i) + p.rows * head_dim + row));
-#pragma unroll 8
-        for (int i = 0; i < pc.y; ++i) {
-          const float* s = piece_of(p, floats, pc.x, i) + p.rows * head_dim + row;
-          x.y = fmaf(__ldcg(s + p.rows), ex2(__ldcg(s) - x.x), x.y);
-        }
-        x.x -= kPagedShift;
-      }
-      x.y = x.y == 0.f ? 0.f : 1.f / x.y;
-      s_ml[h] = x;
-    }
-    __syncthreads();
-    const float* logits = p.logits + ((long long)pair * p.g + h0) * p.logit_row + first;
-#pragma unroll 4
-    for (int h = 0; h < n; ++h) {
-      const float2 ml = s_ml[h];
+  float old[4], w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = i * kThreads + threadIdx.x;
-        if (first + s < len) w[i] += ex2(__ldcg(logits + h * p.logit_row + s) - ml.x) * ml.y;
+  for (int i = 0; i < 4; ++i) old[i] = slot0 + i < min(len, c.score_slots) ? scores[slot0 + i] : 0.f;
+  for (int h0 = 0; h0 < p.g; h0 += 8) {
+    const float* logits = p.logits + ((long long)pair * p.g + h0) * p.logit_row + slot0;
+    float4 x[8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (slot0 < len && h0 + h < p.g) x[h] = __ldcg(reinterpret_cast<const float4*>(logits + h * p.logit_row));
+    __syncthreads();
+    if (h0 + warp < p.g) {
+      const int qi = (h0 + warp) / p.rows, row = h0 + warp - qi * p.rows;
+      const int2 pc = joined ? __ldcg(p.pieces + pair * p.qt + qi) : make_int2(0, 1);
+      float2 ml;
+      if (pc.y == 1) {
+        ml = __ldcg(p.ml + (size_t)pair * p.g + h0 + warp);
+      } else {
+        float m = kNegBig, l = 0.f;
+        for (int i = lane; i < pc.y; i += 32) {
+          const float* s = piece_of(p, floats, pc.x, i) + p.rows * head_dim + row;
+          const float mi = __ldcg(s), li = __ldcg(s + p.rows), top = fmaxf(m, mi);
+          l = l * ex2(m - top) + li * ex2(mi - top);
+          m = top;
+        }
+#pragma unroll
+        for (int s = 16; s >= 1; s >>= 1) {
+          const float mi = __shfl_xor_sync(0xffffffffu, m, s), li = __shfl_xor_sync(0xffffffffu, l, s), top = fmaxf(m, mi);
+          l = l * ex2(m - top) + li * ex2(mi - top);
+          m = top;
+        }
+        ml = make_float2(m - kPagedShift, l);
       }
+      if (lane == 0) s_ml[warp] = make_float2(ml.x, ml.y == 0.f ? 0.f : 1.f / ml.y);
     }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (slot0 < len && h0 + h < p.g) {
+        const float2 ml = s_ml[h];
+        w[0] += ex2(x[h].x - ml.x) * ml.y;
+        w[1] += ex2(x[h].y - ml.x) * ml.y;
+        w[2] += ex2(x[h].z - ml.x) * ml.y;
+        w[3] += ex2(x[h].w - ml.x) * ml.y;
+      }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int slot = first + i * kThreads + threadIdx.x;
+    const int slot = slot0 + i;
     if (slot >= len) continue;
     if (slot >= c.score_slots) paged_flag(c, kPagedBadScores);
     else if (p.k_new && slot == len - 1) scores[slot] = w[i];        // the token being appended has had none before
-    else scores[slot] += w[i];
+    else scores[slot] = old[i] + w[i];
   }
 }
 
@@ -237,7 +250,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads) ssd_paged_join_kernel(const __grid_constant__ JoinParams p) {
   pdl_wait_predecessor();
   pdl_allow_successor();
-  if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units);
+  if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units, p.join_blocks);
   else add_weights(p.d, blockIdx.x - p.join_blocks, p.blocks_per_pair, D, p.join_blocks > 0);
 }
 
@@ -541,15 +554,17 @@ struct Workspace {
   size_t partial, pieces, ml, logits, bytes;
 };
 
+long long logit_row(int cap) { return ((long long)cap + 3) / 4 * 4; }         // whole float4s
+
 Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate, int sms) {
   const int rows = paged_rows(g);
   const size_t heads = (size_t)v.n_seqs * v.H * g;
   Workspace w;
-  w.partial = align_up(paged_max_workers(sms) * 4);
+  w.partial = align_up((size_t)sms * 4);
   w.pieces = align_up(w.partial + paged_max_workers(sms) * 2 * paged_part_floats(rows, head_dim) * 4);
   w.ml = align_up(w.pieces + (size_t)v.n_seqs * v.H * ((g + rows - 1) / rows) * 8);
   w.logits = align_up(w.ml + (accumulate ? heads * 8 : 0));
-  w.bytes = w.logits + (accumulate ? heads * (size_t)v.cap * 4 : 0);
+  w.bytes = w.logits + (accumulate ? heads * (size_t)logit_row(v.cap) * 4 : 0);
   return w;
 }
 
@@ -603,7 +618,7 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   if (a->accumulate) {
     p.ml = reinterpret_cast<float2*>(ws + w.ml);
     p.logits = reinterpret_cast<float*>(ws + w.logits);
-    p.logit_row = p.c.cap;
+    p.logit_row = logit_row(p.c.cap);
   }
   const float scale = a->softmax_scale > 0.f ? a->softmax_scale : 1.f / std::sqrt((float)kv->head_dim);
   p.scale_log2 = scale * 1.44269504088896340736f;

@@ -145,8 +145,8 @@ struct PagedDecodeParams {
   float* logits;            // weights wanted: [n_seqs * H * g, logit_row]; else null
   float2* ml;               // weights wanted: [n_seqs * H * g] (max, sum)
   long long logit_row;
-  uint32_t* counters;       // [workers], zero between launches
-  int2* pieces;             // [n_seqs * H * qt]: the first worker that has a piece of the head, and how many have
+  uint32_t* counters;       // [thread blocks] pieces done (few heads), zero between launches
+  int2* pieces;             // [n_seqs * H * qt]: the first worker that has a piece of the head, and how many have (many heads)
   float* partial;           // [workers][2][paged_part_floats(rows, D)]
   float scale_log2;
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together

@@ -3,7 +3,9 @@
 
 namespace ssd {
 
-size_t paged_max_workers(int sms) { return (size_t)sms * 16; }
+size_t paged_max_workers(int sms) {
+  return (size_t)sms * (SSD_PAGED_WARPS8 > SSD_PAGED_WARPS16 ? SSD_PAGED_WARPS8 : SSD_PAGED_WARPS16);
+}
 
 cudaError_t launch_paged_decode_16(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st) {
   if (p.bf16)

@@ -9,7 +9,10 @@
 // launch, from the lengths that the launch finds on the device.  A warp runs through the heads of its share without ever
 // meeting another; of a head that a share's border cuts it leaves a piece, (O, m, l), and a second launch joins the pieces
 // (ssd_paged_join_kernel).  Joining them here, by whoever completes the last one, was 48 us slower at 16 x 8 heads of up to
-// 32768 slots: one warp merged 15 pieces of 8 query heads while the others were done.
+// 32768 slots: one warp merged 15 pieces of 8 query heads while the others were done.  SMs differ by some 15% in how fast
+// their warps are served, but handing out the last eighth of the stream from a counter, in segments of three tiles and
+// more, cost more than it gave (16 x 32 E4M3 heads of up to 4224 slots 91 -> 97 us, 16 x 8 heads of up to 32768 201 -> 221):
+// every segment pays for finding its place, loading q and leaving a piece.
 // Few heads (kCta): a piece is a run of tiles of one head for a whole thread block, whose warps take them in turn and merge
 // in shared memory.  The pieces of a head meet in global memory, where the thread block that completes the last one
 // (a counter, kept under the worker of the head's first piece) joins them: one launch, for the calls whose latency counts.
@@ -38,17 +41,16 @@ namespace ssd {
 namespace paged {
 
 
-#ifndef SSD_PAGED_WARPS1
-#define SSD_PAGED_WARPS1 12
-#define SSD_PAGED_STAGES1 2
-#define SSD_PAGED_WARPS2 8
-#define SSD_PAGED_STAGES2 3
+#ifndef SSD_PAGED_WARPS16
+#define SSD_PAGED_WARPS16 8
+#define SSD_PAGED_WARPS8 12
+#define SSD_PAGED_STAGES 2
 #endif
 template <int D, int kFmt, int kNt>
 struct Geo {
-  static constexpr int kWarps = kNt == 1 ? SSD_PAGED_WARPS1 : SSD_PAGED_WARPS2;
+  static constexpr int kWarps = kFmt == kPagedE4m3 && kNt == 1 ? SSD_PAGED_WARPS8 : SSD_PAGED_WARPS16;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kStages = kNt == 1 ? SSD_PAGED_STAGES1 : SSD_PAGED_STAGES2;
+  static constexpr int kStages = SSD_PAGED_STAGES;
   static constexpr int kRow = kFmt == kPagedE4m3 ? D : 2 * D;      // bytes of a row in a page
   static constexpr int kTile = 4096 / kRow;                        // keys of a tile
   static constexpr int kCpr = kRow / 16;                           // 16-byte chunks of a row
@@ -232,16 +234,23 @@ struct Worker {
   }
 
   // ---------------------------------------------------------------- loading
-  // Looks up the rows of a tile (this lane's ones) in the table; the loads' latency passes during the tile before.
+  // Looks up a tile's rows in the table, before the tile is issued: the loads' latency passes during the tile before.
+  // Where tiles lie in one page each, lane i holds the page of the i-th tile from the one that was looked up last (`step`
+  // tiles apart), so the table is read once in 32 tiles; else lane i works out the rows i, i + 32 of the one tile.
   struct Rows {
     int page[G::kRpl], row[G::kRpl];
+    int k;                                                   // the lane that has the tile's page
   };
-  __device__ __forceinline__ void look_up(const Place& at, int seq, int head, Rows& r) const {
+  __device__ __forceinline__ void look_up(const Place& at, int seq, int head, int step, bool fresh, Rows& r) const {
     const int32_t* table = paged_table(p.c, seq, head);
     if (p.whole_tiles) {
-      int index;
-      paged_split(p.c, at.t * G::kTile, index, r.row[0]);
-      r.page[0] = table[index];
+      r.k = fresh || r.k == 31 ? 0 : r.k + 1;
+      if (r.k == 0) {
+        const int slot = (at.t + lane * step) * G::kTile;
+        int index, row;
+        paged_split(p.c, slot, index, row);
+        r.page[0] = slot < at.len ? table[index] : -1;
+      }
       return;
     }
 #pragma unroll
@@ -272,9 +281,12 @@ struct Worker {
     constexpr int kRpi = 32 / G::kCpr;                       // rows that one copy instruction of the warp brings
     const int chunk = lane % G::kCpr;
     if (p.whole_tiles) {                                     // a tile lies in one page: one address, and strides
-      const bool ok = (uint32_t)r.page[0] < (uint32_t)c.n_pages;             // the same for the whole warp
+      const int page = __shfl_sync(0xffffffffu, r.page[0], r.k);
+      int index, row0;
+      paged_split(c, at.t * G::kTile, index, row0);
+      const bool ok = (uint32_t)page < (uint32_t)c.n_pages;
       if (!ok) paged_flag(c, kPagedBadPage);
-      const long long first = ok ? r.page[0] * c.page_b + head * c.head_b + r.row[0] * c.slot_b : 0;
+      const long long first = ok ? page * c.page_b + head * c.head_b + row0 * c.slot_b : 0;
       const int skip = fused && last < G::kTile ? last : G::kTile;           // rows from here on are not copied ..
       const int held = min(last + 1, G::kTile);                              // .. and rows from here on do not exist
       const char* k = c.k + first + (lane / G::kCpr) * c.slot_b + chunk * 16;
@@ -301,7 +313,7 @@ struct Worker {
         }
       }
       if constexpr (kFmt == kPagedE4m3) {
-        const long long so = ok ? r.page[0] * c.sc_page + head * c.sc_head + r.row[0] * c.sc_slot : 0;
+        const long long so = ok ? page * c.sc_page + head * c.sc_head + row0 * c.sc_slot : 0;
 #pragma unroll
         for (int i = 0; i < G::kRpl; ++i) {
           const int local = i * 32 + lane;
@@ -313,7 +325,7 @@ struct Worker {
           }
         }
       }
-      if (skip < G::kTile) put_new(at, seq, head, qi, base, last, r.page[0], r.row[0] + last);
+      if (skip < G::kTile) put_new(at, seq, head, qi, base, last, page, row0 + last);
       if (lane == 0) {
         uint2* mask = reinterpret_cast<uint2*>(ring_ptr + stage * G::kStage + G::kMaskAt);
         const uint32_t lo = held >= 32 ? ~0u : (1u << held) - 1u, hi = held <= 32 ? 0u : (held >= 64 ? ~0u : (1u << (held - 32)) - 1u);
@@ -703,28 +715,42 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
   // a worker's pieces of heads that it shares: the one that starts in its share, and the one that does not
   auto partial_of = [&](uint32_t who, bool starts) { return p.partial + ((size_t)who * 2 + (starts ? 1 : 0)) * part_floats; };
   W w(p, lane, ring + warp * G::kRing);
-  auto steps = [&](int n) { return n > 0 ? n + kStages - 1 : 0; };
 
   if constexpr (!kCta) {
-    // ---- the stream of tiles: sums over runs of (sequence, head, group), one run per thread
-    const int run = (n_vp + kThreads - 1) / kThreads;
-    const int lo = min(n_vp, tid * run), hi = min(n_vp, lo + run);
+    // ---- the stream of tiles.  An entry is a run of heads of one length: those of a sequence, or the groups of a head.
+    const bool shared = c.n_head == 0;
+    const int mult = shared ? c.H * p.qt : p.qt;
+    const int n_entries = shared ? c.n_seqs : c.n_seqs * c.H;
+    auto entry_length = [&](int e) {
+      if (shared) return paged_length(c, e, 0);
+      const int seq = (int)p.by_heads.div((uint32_t)e);
+      return paged_length(c, seq, e - seq * c.H);
+    };
+    const int run = (n_entries + kThreads - 1) / kThreads;   // entries of a thread
+    const int lo = min(n_entries, tid * run), hi = min(n_entries, lo + run);
     uint32_t sum = 0u, total;
 #pragma unroll 4
-    for (int i = lo; i < hi; ++i) {
-      const int len = length_of(i);
-      sum += tiles_of(len);
-      if (len == 0 && (uint32_t)i % gridDim.x == blockIdx.x) {
-        zeros(i);
-        p.pieces[i] = make_int2(0, 0);
+    for (int e = lo; e < hi; ++e) {
+      const int len = entry_length(e);
+      sum += tiles_of(len) * mult;
+      if (len == 0) {
+        const int skew = e * mult % (int)gridDim.x;          // head v is the business of thread block v mod gridDim
+        for (int v = e * mult + ((int)blockIdx.x - skew + (skew > (int)blockIdx.x ? (int)gridDim.x : 0)); v < (e + 1) * mult; v += gridDim.x) {
+          zeros(v);
+          p.pieces[v] = make_int2(0, 0);
+        }
       }
     }
     s_pref[tid] = block_scan<kThreads>(sum, s_warp, total);
     __syncthreads();
     const uint32_t workers = gridDim.x * kWarps, worker = blockIdx.x * kWarps + warp;
-    uint32_t share = (total + workers - 1) / workers;
-    if (share == 0u) share = 1u;
-    const uint32_t first = worker * share, end = min(total, first + share);
+    const uint32_t share = total / workers, longer = total % workers;       // the first `longer` workers have one more
+    auto first_of = [&](uint32_t k) { return k * share + min(k, longer); };
+    auto worker_of = [&](uint32_t x) {
+      const uint32_t y = longer * (share + 1);
+      return x < y ? x / (share + 1) : longer + (x - y) / share;
+    };
+    const uint32_t first = first_of(worker), end = first_of(worker + 1);
     if (first >= end) return;
 
     // ---- the head that holds the worker's first tile
@@ -735,10 +761,10 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
 #pragma unroll
       for (int i = 0; i < kThreads / 32; ++i) n += s_pref[i * 32 + lane] <= first;
       n = __reduce_add_sync(0xffffffffu, n);                 // runs that begin at or before it: the last of them has it
-      vp = (n - 1) * run;
+      int e = (n - 1) * run;
       at = s_pref[n - 1];
-      for (;;) {                                             // ends: `first` lies inside this run
-        const uint32_t mine = vp + lane < n_vp ? tiles_of(length_of(vp + lane)) : 0u;
+      while (run > 1) {                                      // ends: the tile lies inside this run
+        const uint32_t mine = e + lane < n_entries ? tiles_of(entry_length(e + lane)) * mult : 0u;
         uint32_t x = mine;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
@@ -749,13 +775,16 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
         if (over) {
           const int who = __ffs(over) - 1;
           at += __shfl_sync(0xffffffffu, x - mine, who);
-          vp += who;
+          e += who;
           break;
         }
         at += __shfl_sync(0xffffffffu, x, 31);
-        vp += 32;
-        if (vp >= n_vp) return;                              // cannot be: the tile exists
+        e += 32;
+        if (e >= n_entries) return;                          // cannot be: the tile exists
       }
+      const uint32_t n_tiles = tiles_of(entry_length(e)), nth = (first - at) / n_tiles;
+      vp = e * mult + (int)nth;
+      at += nth * n_tiles;
     }
     // one stream of tiles per warp, across heads: `ahead` issues copies, `now` consumes
     auto enter = [&](Place& pl, int v, uint32_t start) {     // the worker's part of a head whose first tile is `start`
@@ -781,17 +810,18 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     int seq_a, head_a, qi_a, seq, head, qi;
     name(ahead.vp, seq_a, head_a, qi_a);
     seq = seq_a; head = head_a; qi = qi_a;
-    w.look_up(ahead, seq_a, head_a, rows);
+    w.look_up(ahead, seq_a, head_a, 1, true, rows);
     w.begin(seq, head, qi);
     const int n = (int)(end - first);
     int in = 0, out = 0;                                     // stages
 #pragma unroll 1
-    for (int i = 0; i < steps(n); ++i) {
+    for (int i = 0; i < n + kStages - 1; ++i) {
       if (i < n) {
         w.issue(ahead, seq_a, head_a, qi_a, in, rows);
         if (i + 1 < n) {
-          if (advance(ahead, start_a)) name(ahead.vp, seq_a, head_a, qi_a);
-          w.look_up(ahead, seq_a, head_a, rows);
+          const bool fresh = advance(ahead, start_a);
+          if (fresh) name(ahead.vp, seq_a, head_a, qi_a);
+          w.look_up(ahead, seq_a, head_a, 1, fresh, rows);
         }
         if (++in == kStages) in = 0;
       }
@@ -804,7 +834,7 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       if (++out == kStages) out = 0;
       if (now.t + 1 == now.end) {
         w.close();
-        const uint32_t w0 = start_n / share, w1 = (start_n + tiles_of(now.len) - 1) / share;
+        const uint32_t w0 = worker_of(start_n), w1 = worker_of(start_n + tiles_of(now.len) - 1);
         if (lane == 0 && worker == w0) p.pieces[now.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
         if (w0 == w1) w.write_out(seq, head, qi);
         else w.write_state(partial_of(worker, worker == w0), D, min(p.g - qi * p.rows, p.rows));
@@ -857,15 +887,15 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       pl.t = now.t = t0 + warp;
       const int n = pl.end > pl.t ? (pl.end - pl.t + kWarps - 1) / kWarps : 0;
       typename W::Rows rows;
-      if (n > 0) w.look_up(pl, seq, head, rows);
+      if (n > 0) w.look_up(pl, seq, head, kWarps, true, rows);
       w.begin(seq, head, qi);
       int in = 0, out = 0;
 #pragma unroll 1
-      for (int i = 0; i < steps(n); ++i) {
+      for (int i = 0; n > 0 && i < n + kStages - 1; ++i) {
         if (i < n) {
           w.issue(pl, seq, head, qi, in, rows);
           pl.t += kWarps;
-          if (i + 1 < n) w.look_up(pl, seq, head, rows);
+          if (i + 1 < n) w.look_up(pl, seq, head, kWarps, false, rows);
           if (++in == kStages) in = 0;
         }
         cp_commit();
