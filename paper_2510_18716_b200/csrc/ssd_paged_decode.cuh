@@ -717,7 +717,8 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
   W w(p, lane, ring + warp * G::kRing);
 
   if constexpr (!kCta) {
-    // ---- the stream of tiles.  An entry is a run of heads of one length: those of a sequence, or the groups of a head.
+    // ---- the stream.  An entry is a run of heads of one length: those of a sequence, or the groups of a head.  A head counts
+    // for its tiles and one more, which is what beginning and ending it costs a warp.
     const bool shared = c.n_head == 0;
     const int mult = shared ? c.H * p.qt : p.qt;
     const int n_entries = shared ? c.n_seqs : c.n_seqs * c.H;
@@ -726,13 +727,14 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       const int seq = (int)p.by_heads.div((uint32_t)e);
       return paged_length(c, seq, e - seq * c.H);
     };
+    auto units_of = [&](int len) { return len > 0 ? tiles_of(len) + 1u : 0u; };
     const int run = (n_entries + kThreads - 1) / kThreads;   // entries of a thread
     const int lo = min(n_entries, tid * run), hi = min(n_entries, lo + run);
     uint32_t sum = 0u, total;
 #pragma unroll 4
     for (int e = lo; e < hi; ++e) {
       const int len = entry_length(e);
-      sum += tiles_of(len) * mult;
+      sum += units_of(len) * mult;
       if (len == 0) {
         const int skew = e * mult % (int)gridDim.x;          // head v is the business of thread block v mod gridDim
         for (int v = e * mult + ((int)blockIdx.x - skew + (skew > (int)blockIdx.x ? (int)gridDim.x : 0)); v < (e + 1) * mult; v += gridDim.x) {
@@ -753,18 +755,48 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     const uint32_t first = first_of(worker), end = first_of(worker + 1);
     if (first >= end) return;
 
-    // ---- the head that holds the worker's first tile
-    int vp;
-    uint32_t at;                                             // tiles before vp
+    // A warp's copies are issued at one place, `ahead`, and consumed at another, `now`.
+    struct Cursor {
+      Place pl;
+      uint32_t start;                                        // of the head, in the stream
+      int seq, head, qi;
+    };
+    auto enter = [&](Cursor& k, int v, uint32_t start) {     // whether any tile of this head is the worker's
+      name(v, k.seq, k.head, k.qi);
+      k.pl.vp = v;
+      k.pl.len = paged_length(c, k.seq, k.head);
+      k.start = start;
+      const uint32_t n = tiles_of(k.pl.len);
+      k.pl.t = first > start ? (int)(first - start) : 0;
+      k.pl.end = (int)min(n, end - start);
+      return k.pl.t < k.pl.end;
+    };
+    auto next = [&](Cursor& k) {                             // to the next head; false: there is none
+      do {
+        const uint32_t start = k.start + units_of(k.pl.len);
+        if (start >= end) return false;
+        if (enter(k, k.pl.vp + 1, start)) return true;
+      } while (true);
+    };
+    auto touch = [&](const Cursor& k) {                      // the queries will be in L1 when the head begins
+      constexpr int kLines = D / 64;
+      const int h = lane / kLines;
+      if (h < min(p.g - k.qi * p.rows, p.rows)) {
+        const char* q = p.q + k.seq * p.q_seq + ((long long)k.head * p.g + k.qi * p.rows + h) * p.q_head + lane % kLines * 128;
+        asm volatile("{\n.reg .b32 t;\nld.global.ca.b32 t, [%0];\n}\n" ::"l"(q) : "memory");
+      }
+    };
+    Cursor ahead;
+    bool more;
     {
       int n = 0;
 #pragma unroll
       for (int i = 0; i < kThreads / 32; ++i) n += s_pref[i * 32 + lane] <= first;
       n = __reduce_add_sync(0xffffffffu, n);                 // runs that begin at or before it: the last of them has it
       int e = (n - 1) * run;
-      at = s_pref[n - 1];
-      while (run > 1) {                                      // ends: the tile lies inside this run
-        const uint32_t mine = e + lane < n_entries ? tiles_of(entry_length(e + lane)) * mult : 0u;
+      uint32_t at = s_pref[n - 1];                           // units before entry e
+      while (run > 1) {                                      // ends: `first` lies inside this run
+        const uint32_t mine = e + lane < n_entries ? units_of(entry_length(e + lane)) * mult : 0u;
         uint32_t x = mine;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
@@ -780,68 +812,49 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
         }
         at += __shfl_sync(0xffffffffu, x, 31);
         e += 32;
-        if (e >= n_entries) return;                          // cannot be: the tile exists
+        if (e >= n_entries) return;                          // cannot be: the unit exists
       }
-      const uint32_t n_tiles = tiles_of(entry_length(e)), nth = (first - at) / n_tiles;
-      vp = e * mult + (int)nth;
-      at += nth * n_tiles;
+      const uint32_t units = units_of(entry_length(e)), nth = (first - at) / units;
+      more = enter(ahead, e * mult + (int)nth, at + nth * units) || next(ahead);
     }
-    // one stream of tiles per warp, across heads: `ahead` issues copies, `now` consumes
-    auto enter = [&](Place& pl, int v, uint32_t start) {     // the worker's part of a head whose first tile is `start`
-      pl.vp = v;
-      pl.len = length_of(v);
-      const uint32_t n = tiles_of(pl.len);
-      pl.t = first > start ? (int)(first - start) : 0;
-      pl.end = (int)min(n, end - start);
-    };
-    auto advance = [&](Place& pl, uint32_t& start) {         // to the next tile; true: it is another head's
-      if (++pl.t < pl.end) return false;
-      do {
-        start += tiles_of(pl.len);
-        enter(pl, pl.vp + 1, start);
-      } while (pl.len == 0);
-      return true;
-    };
-    uint32_t start_a = at, start_n = at;
-    Place ahead, now;
+    if (!more) return;
     typename W::Rows rows;
-    enter(ahead, vp, start_a);
-    now = ahead;
-    int seq_a, head_a, qi_a, seq, head, qi;
-    name(ahead.vp, seq_a, head_a, qi_a);
-    seq = seq_a; head = head_a; qi = qi_a;
-    w.look_up(ahead, seq_a, head_a, 1, true, rows);
-    w.begin(seq, head, qi);
-    const int n = (int)(end - first);
-    int in = 0, out = 0;                                     // stages
+    w.look_up(ahead.pl, ahead.seq, ahead.head, 1, true, rows);
+    Cursor now = ahead;
+    w.begin(now.seq, now.head, now.qi);
+    int in = 0, out = 0, open = 0;                           // stages, and tiles issued and not consumed
 #pragma unroll 1
-    for (int i = 0; i < n + kStages - 1; ++i) {
-      if (i < n) {
-        w.issue(ahead, seq_a, head_a, qi_a, in, rows);
-        if (i + 1 < n) {
-          const bool fresh = advance(ahead, start_a);
-          if (fresh) name(ahead.vp, seq_a, head_a, qi_a);
-          w.look_up(ahead, seq_a, head_a, 1, fresh, rows);
-        }
+    for (int i = 0;; ++i) {
+      if (more) {
+        w.issue(ahead.pl, ahead.seq, ahead.head, ahead.qi, in, rows);
         if (++in == kStages) in = 0;
+        ++open;
+        const bool same = ++ahead.pl.t < ahead.pl.end;
+        if (!same) {
+          more = next(ahead);
+          if (more) touch(ahead);
+        }
+        if (more) w.look_up(ahead.pl, ahead.seq, ahead.head, 1, !same, rows);
       }
       cp_commit();
       if (i < kStages - 1) continue;
+      if (open == 0) break;
       cp_wait<kStages - 1>();
       __syncwarp();
-      w.consume(now, seq, head, qi, out);
+      w.consume(now.pl, now.seq, now.head, now.qi, out);
       __syncwarp();
       if (++out == kStages) out = 0;
-      if (now.t + 1 == now.end) {
+      --open;
+      if (++now.pl.t == now.pl.end) {
         w.close();
-        const uint32_t w0 = worker_of(start_n), w1 = worker_of(start_n + tiles_of(now.len) - 1);
-        if (lane == 0 && worker == w0) p.pieces[now.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
-        if (w0 == w1) w.write_out(seq, head, qi);
-        else w.write_state(partial_of(worker, worker == w0), D, min(p.g - qi * p.rows, p.rows));
-      }
-      if (i < n + kStages - 2 && advance(now, start_n)) {
-        name(now.vp, seq, head, qi);
-        w.begin(seq, head, qi);
+        const uint32_t w0 = worker_of(now.start), w1 = worker_of(now.start + tiles_of(now.pl.len) - 1);
+        if (lane == 0 && worker == w0) p.pieces[now.pl.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
+        if (w0 == w1) w.write_out(now.seq, now.head, now.qi);
+        else w.write_state(partial_of(worker, worker == w0), D, min(p.g - now.qi * p.rows, p.rows));
+        if (open > 0 || more) {
+          next(now);
+          w.begin(now.seq, now.head, now.qi);
+        }
       }
     }
   } else {
