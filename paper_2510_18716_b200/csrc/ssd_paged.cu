@@ -33,24 +33,27 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
   pdl_allow_successor();
   const int token = (int)(item / groups), head0 = (int)(item % groups) * kAppendHeads;
   if (token >= p.n_tokens) return;
-  int seq = token, ago = 1;
-  if (p.cu) {                                       // the last sequence that begins at or before the token
-    int a = 0, b = c.n_seqs;
-    while (a < b) {
-      const int m = (a + b) >> 1;
-      if (p.cu[m] <= token) a = m + 1; else b = m;
-    }
-    seq = a - 1;
-    if (seq < 0) return;
-    ago = p.cu[seq + 1] - token;            // 1 for a sequence's newest token
-    if (ago <= 0) return;
-  }
-  uint4 raw[kIters];
+  uint4 raw[kIters];                                // on the way while the token's place is looked for
 #pragma unroll
   for (int it = 0; it < kIters; ++it) {
     const int r = it * kRows + lane / kL, head = head0 + (r >> 1);
     raw[it] = make_uint4(0u, 0u, 0u, 0u);
     if (head < c.H) raw[it] = reinterpret_cast<const uint4*>((r & 1 ? p.v_new : p.k_new) + token * p.token_b + head * p.head_b)[lane % kL];
+  }
+  int seq = token, ago = 1;
+  if (p.cu) {                                       // the last sequence that begins at or before the token, 32 probes at a time
+    int a = 0, n = c.n_seqs;                        // cu[a - 1] <= token < cu[a + n], as far as those exist
+    while (n > 0) {
+      const int step = (n + 31) / 32, at = a + min(n, (lane + 1) * step) - 1;
+      const int k = __popc(__ballot_sync(0xffffffffu, p.cu[at] <= token));   // cu ascends: probes 0 .. k - 1
+      const int from = min(n, k * step), to = min(n, (k + 1) * step - 1);
+      a += from;
+      n = k == 32 ? 0 : to - from;
+    }
+    seq = a - 1;
+    if (seq < 0) return;
+    ago = p.cu[seq + 1] - token;                    // 1 for a sequence's newest token
+    if (ago <= 0) return;
   }
 #pragma unroll
   for (int it = 0; it < kIters; ++it) {
@@ -260,7 +263,6 @@ struct EvictParams {
   int in_place, dst_scores, prefix, kept_cols;
   int32_t* kept;
   int32_t* counts;
-  int keys_cap;                    // candidates whose keys fit in shared memory
   int32_t budget[kMaxHeads], recent[kMaxHeads];
 };
 
@@ -271,201 +273,302 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// One thread block per (sequence, head): the budget-th largest key by digits of 11, 11 and 10 bits from the top (stopping
-// as soon as a digit's bin is taken whole), then the candidates above it and the first ones equal to it, in order.
-template <int kT>
-__global__ void __launch_bounds__(kT) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
-  constexpr int kBins = 2048, kW = kT / 32, kPer = kBins / kT;
-  extern __shared__ uint32_t s_keys[];
-  __shared__ uint32_t s_hist[kBins];
-  __shared__ uint32_t s_warp[kW], s_warp2[kW];
-  __shared__ uint32_t s_bin, s_need, s_whole;
-  const PagedView& c = p.src;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int pair = blockIdx.x, seq = pair / c.H, head = pair - seq * c.H;
-  pdl_wait_predecessor();
-  pdl_allow_successor();
-  const int n = paged_length(c, seq, head);
-  const int budget = p.budget[head], recent = p.recent[head], keep = p.prefix + budget + recent;
-  int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
-  const float* scores = paged_scores(c, seq, head);
-  const bool all = n <= keep;
-  const int count = all ? n : keep;
-
-  if (all) {
-    for (int j = tid; j < n; j += kT) kept[j] = j;
-  } else {
-    for (int j = tid; j < p.prefix; j += kT) kept[j] = j;
-    for (int j = tid; j < recent; j += kT) kept[p.prefix + budget + j] = n - recent + j;
-    const int nc = n - recent - p.prefix;                    // candidates: more than the budget
-    auto score_of = [&](int i) {
-      const int slot = p.prefix + i;
-      if (slot < c.score_slots) return scores[slot];
-      paged_flag(c, kPagedBadScores);
-      return 0.f;
-    };
-    const bool cached = nc <= p.keys_cap;
-    if (cached)
-      for (int i = tid; i < nc; i += kT) s_keys[i] = score_key(score_of(i));
-    auto key_of = [&](int i) { return cached ? s_keys[i] : score_key(score_of(i)); };
-    uint32_t prefix = 0u, mask = 0u, need = (uint32_t)budget;
-    bool whole = false;                                      // every key with this prefix is taken
-    for (int digit = 0; budget > 0 && digit < 3 && !whole; ++digit) {
-      const int shift = digit == 0 ? 21 : (digit == 1 ? 10 : 0);
-      const uint32_t width = digit == 2 ? 1023u : 2047u;
-      for (int b = tid; b < kBins; b += kT) s_hist[b] = 0u;
-      __syncthreads();
-      for (int i = tid; i < nc; i += kT) {
-        const uint32_t k = key_of(i);
-        if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & width], 1u);
-      }
-      __syncthreads();
-      // bins from the top: thread t has bins kBins - 1 - t * kPer and below
-      uint32_t own[kPer], sum = 0u;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        own[i] = s_hist[kBins - 1 - tid * kPer - i];
-        sum += own[i];
-      }
-      uint32_t inc = sum;
-#pragma unroll
-      for (int s = 1; s < 32; s <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, inc, s);
-        if (lane >= s) inc += x;
-      }
-      if (lane == 31) s_warp[warp] = inc;
-      __syncthreads();
-      uint32_t before = inc - sum;
-      for (int w = 0; w < warp; ++w) before += s_warp[w];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (before < need && need <= before + own[i]) {
-          s_bin = kBins - 1 - tid * kPer - i;
-          s_need = need - before;
-          s_whole = need == before + own[i];
-        }
-        before += own[i];
-      }
-      __syncthreads();
-      prefix |= s_bin << shift;
-      mask |= width << shift;
-      need = s_need;
-      whole = s_whole != 0u;
-    }
-    // `need` of the candidates whose key has this prefix are taken (the first ones), and all above
-    if (budget > 0) {
-      __syncthreads();                                       // the keys, where no digit was looked at
-      const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
-      const int a = min(nc, warp * seg), b = min(nc, a + seg);
-      uint32_t above = 0u, equal = 0u;
-      for (int i0 = a; i0 < b; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t k = i < b ? key_of(i) & mask : 0u;
-        above += __popc(__ballot_sync(0xffffffffu, i < b && k > prefix));
-        equal += __popc(__ballot_sync(0xffffffffu, i < b && k == prefix));
-      }
-      if (lane == 0) { s_warp[warp] = above; s_warp2[warp] = equal; }
-      __syncthreads();
-      uint32_t g = 0u, e = 0u;
-      for (int w = 0; w < warp; ++w) { g += s_warp[w]; e += s_warp2[w]; }
-      const unsigned below = (1u << lane) - 1u;
-      for (int i0 = a; i0 < b; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t k = i < b ? key_of(i) & mask : 0u;
-        const unsigned mg = __ballot_sync(0xffffffffu, i < b && k > prefix);
-        const unsigned me = __ballot_sync(0xffffffffu, i < b && k == prefix);
-        const uint32_t gi = g + __popc(mg & below), ei = e + __popc(me & below);
-        if (i < b && (k > prefix || (k == prefix && ei < need))) kept[p.prefix + gi + min(ei, need)] = p.prefix + i;
-        g += __popc(mg);
-        e += __popc(me);
-      }
+// The need-th largest of the keys that the threads of a group (a warp, or a thread block) hold, bit by bit from the top:
+// a bit is set iff at least `need` keys are not below the value with it.  `count(k)`: how many of the group's keys are >= k.
+// Returns the value; whole: exactly `need` keys are at or above it.
+template <class F>
+__device__ __forceinline__ uint32_t nth_key(uint32_t need, F count, bool& whole) {
+  uint32_t t = 0u;
+  whole = false;
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+    const uint32_t n = count(t | bit);
+    if (n >= need) t |= bit;
+    if (n == need) {
+      whole = true;
+      break;
     }
   }
-  for (int j = count + tid; j < p.kept_cols; j += kT) kept[j] = -1;
-  if (tid == 0) p.counts[pair] = count;
-  if (!p.dst_scores || (all && p.in_place)) return;
-  // the scores travel with their tokens; in place, a slot's value is read before it is overwritten (sources lie at or
-  // above their destinations, so a round's writes touch nothing that a later round reads)
-  float* to = paged_scores(p.dst, seq, head);
-  __syncthreads();
-  for (int j0 = 0; j0 < count; j0 += kT) {
-    const int j = j0 + tid;
-    float x = 0.f;
-    if (j < count) {
-      const int s = kept[j];
-      if (s < c.score_slots) x = scores[s];
+  return t;
+}
+
+// What a (sequence, head) keeps besides the candidates chosen, and the number of them all.
+struct EvictHead {
+  int n, budget, recent, count;
+  bool all;
+  int32_t* kept;
+  const float* scores;
+  float* to;
+};
+__device__ __forceinline__ EvictHead evict_head(const EvictParams& p, int pair) {
+  EvictHead e;
+  const int seq = pair / p.src.H, head = pair - seq * p.src.H;
+  e.n = paged_length(p.src, seq, head);
+  e.budget = p.budget[head];
+  e.recent = p.recent[head];
+  const int keep = p.prefix + e.budget + e.recent;
+  e.all = e.n <= keep;
+  e.count = e.all ? e.n : keep;
+  e.kept = p.kept + (size_t)pair * p.kept_cols;
+  e.scores = paged_scores(p.src, seq, head);
+  e.to = p.dst_scores && !(e.all && p.in_place) ? paged_scores(p.dst, seq, head) : nullptr;
+  return e;
+}
+__device__ __forceinline__ float evict_score(const EvictParams& p, const EvictHead& e, int slot) {
+  if (slot < p.src.score_slots) return e.scores[slot];
+  paged_flag(p.src, kPagedBadScores);
+  return 0.f;
+}
+// Everything that is not a choice, by kT threads.
+template <int kT>
+__device__ __forceinline__ void list_rest(const EvictParams& p, const EvictHead& e, int pair, int tid) {
+  if (e.all) {
+    for (int j = tid; j < e.n; j += kT) e.kept[j] = j;
+  } else {
+    for (int j = tid; j < p.prefix; j += kT) e.kept[j] = j;
+    for (int j = tid; j < e.recent; j += kT) e.kept[p.prefix + e.budget + j] = e.n - e.recent + j;
+  }
+  for (int j = e.count + tid; j < p.kept_cols; j += kT) e.kept[j] = -1;
+  if (tid == 0) p.counts[pair] = e.count;
+}
+// Four rounds of kT scores travel with their tokens at a time, all read before the first is written.  In place that keeps
+// it right: sources lie at or above their destinations, so what is written here is not read by a later round.
+template <int kT, class S>
+__device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHead& e, int tid, S sync) {
+  if (!e.to) return;
+  sync();                                                    // the list is complete
+  for (int j0 = 0; j0 < e.count; j0 += 4 * kT) {
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + u * kT + tid;
+      x[u] = 0.f;
+      if (j < e.count) {
+        const int s = e.kept[j];
+        if (s < p.src.score_slots) x[u] = e.scores[s];
+      }
     }
-    if (p.in_place) __syncthreads();
-    if (j < count) {
-      if (j < p.dst.score_slots) to[j] = x;
+    if (p.in_place) sync();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + u * kT + tid;
+      if (j >= e.count) continue;
+      if (j < p.dst.score_slots) e.to[j] = x[u];
       else paged_flag(p.dst, kPagedBadScores);
     }
   }
 }
 
+constexpr int kKeys = 32;                                    // keys of a thread
+
+// Tables of up to 1024 slots: a warp per (sequence, head), its keys in registers, no barrier.  (Thread blocks of 256
+// threads with histograms of the keys' digits took 19 us for 64 x 32 heads of up to 640 slots, this 7.)
+__global__ void __launch_bounds__(kThreads) ssd_paged_select_short_kernel(const __grid_constant__ EvictParams p) {
+  const int lane = threadIdx.x & 31;
+  const int pair = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  if (pair >= p.src.n_seqs * p.src.H) return;
+  const EvictHead e = evict_head(p, pair);
+  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
+  const bool choose = !e.all && e.budget > 0;
+  uint32_t key[kKeys];
+  if (choose) {
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) key[r] = r * 32 + lane < nc ? score_key(evict_score(p, e, p.prefix + r * 32 + lane)) : 0u;
+  }
+  list_rest<32>(p, e, pair, lane);
+  if (choose) {
+    bool whole;
+    // keys that do not exist are 0 and are counted only for k == 0, which is not asked for
+    const uint32_t t = nth_key((uint32_t)e.budget, [&](uint32_t k) {
+      uint32_t n = 0u;
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r) n += key[r] >= k;
+      return __reduce_add_sync(0xffffffffu, n);
+    }, whole);
+    // the keys above t, and the first ones equal to it that make up the budget
+    uint32_t above = 0u;
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) above += key[r] > t;
+    above = __reduce_add_sync(0xffffffffu, above);
+    uint32_t need = whole ? 0xffffffffu : (uint32_t)e.budget - above;
+    const unsigned below = (1u << lane) - 1u;
+    uint32_t at = 0u;
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) {
+      const int i = r * 32 + lane;
+      const unsigned equal = __ballot_sync(0xffffffffu, i < nc && key[r] == t);
+      const bool mine = i < nc && (key[r] > t || (key[r] == t && (uint32_t)__popc(equal & below) < need));
+      const unsigned taken = __ballot_sync(0xffffffffu, mine);
+      if (mine) e.kept[p.prefix + at + __popc(taken & below)] = p.prefix + i;
+      at += __popc(taken);
+      need -= min(need, (uint32_t)__popc(equal));
+    }
+  }
+  move_scores<32>(p, e, lane, [] { __syncwarp(); });
+}
+
+// Longer tables: a thread block per (sequence, head).  Up to 32 K candidates in registers, each warp a run of them; beyond,
+// they are read again for every bit.
+__global__ void __launch_bounds__(1024) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kT = 1024, kW = kT / 32;
+  __shared__ uint32_t s_count[2][kW];
+  __shared__ uint32_t s_above[kW], s_equal[kW];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int pair = blockIdx.x;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const EvictHead e = evict_head(p, pair);
+  const int nc = e.n - e.recent - p.prefix;
+  if (!e.all && e.budget > 0) {
+    const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;     // candidates of a warp
+    const int a = min(nc, warp * seg), b = min(nc, a + seg), rounds = seg / 32;
+    const bool held = rounds <= kKeys;
+    uint32_t key[kKeys];
+    auto fetch = [&](int r) {
+      const int i = a + r * 32 + lane;
+      return i < b ? score_key(evict_score(p, e, p.prefix + i)) : 0u;
+    };
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) key[r] = held && r < rounds ? fetch(r) : 0u;
+    list_rest<kT>(p, e, pair, tid);
+    auto each = [&](auto f) {                                // f(round, key) for the rounds of this warp, in order
+      if (held) {
+#pragma unroll
+        for (int r = 0; r < kKeys; ++r)
+          if (r < rounds) f(r, key[r]);
+      } else {
+#pragma unroll 4
+        for (int r = 0; r < rounds; ++r) f(r, fetch(r));
+      }
+    };
+    int turn = 0;
+    bool whole;
+    const uint32_t t = nth_key((uint32_t)e.budget, [&](uint32_t k) {
+      uint32_t n = 0u;
+      each([&](int, uint32_t x) { n += x >= k; });
+      n = __reduce_add_sync(0xffffffffu, n);
+      turn ^= 1;                                             // two sets of counts: one barrier per bit
+      if (lane == 0) s_count[turn][warp] = n;
+      __syncthreads();
+      return __reduce_add_sync(0xffffffffu, s_count[turn][lane]);
+    }, whole);
+    uint32_t above = 0u, equal = 0u;
+    each([&](int r, uint32_t x) {
+      const bool in = a + r * 32 + lane < b;
+      above += in && x > t;
+      equal += in && x == t;
+    });
+    above = __reduce_add_sync(0xffffffffu, above);
+    equal = __reduce_add_sync(0xffffffffu, equal);
+    if (lane == 0) { s_above[warp] = above; s_equal[warp] = equal; }
+    __syncthreads();
+    const uint32_t all_above = __reduce_add_sync(0xffffffffu, s_above[lane]);
+    const uint32_t need = whole ? 0xffffffffu : (uint32_t)e.budget - all_above;              // of the equal ones, the first
+    const uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_equal[lane] : 0u);
+    const uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_above[lane] : 0u);
+    uint32_t at = gt_before + min(eq_before, need), eq = eq_before;
+    const unsigned below = (1u << lane) - 1u;
+    each([&](int r, uint32_t x) {
+      const int i = a + r * 32 + lane;
+      const unsigned same = __ballot_sync(0xffffffffu, i < b && x == t);
+      const bool mine = i < b && (x > t || (x == t && eq + __popc(same & below) < need));
+      const unsigned taken = __ballot_sync(0xffffffffu, mine);
+      if (mine) e.kept[p.prefix + at + __popc(taken & below)] = p.prefix + i;
+      at += __popc(taken);
+      eq += __popc(same);
+    });
+  } else {
+    list_rest<kT>(p, e, pair, tid);
+  }
+  move_scores<kT>(p, e, tid, [] { __syncthreads(); });
+}
+
 // ----------------------------------------------------------------------------- eviction: moving the rows
-// Row j of a head comes from slot kept[j] >= j.  Elsewhere: 2 row bytes / 16 lanes move a token (K and V), and a head's
-// tokens are shared out over gridDim.z thread blocks.  In place: the thread blocks of a head have 64 bytes of every
-// row each (blockIdx.y), so that the order that keeps it right (a round's rows are all read before the first is
-// written; later rounds read only above what it writes) is a matter of one thread block.
+// Token j of a head comes from slot kept[j] >= j.  A warp moves 32 tokens: each lane looks one of them up (source and
+// destination pages) and copies its scales, then 2 row bytes / 16 lanes at a time copy a token's K and V rows.
+// In place, one thread block has 64 bytes of every row of a head (blockIdx.y), in rounds of 256 tokens: all rows of a round
+// are read before the first is written, and later rounds read only above what it writes.
 template <int kRow, bool kInPlace>
-__global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_constant__ EvictParams p) {
+__global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_constant__ EvictParams p, int chunks) {
   constexpr int kCpr = kRow / 16;                            // 16-byte chunks of a row; a token has twice as many
   constexpr int kL = kInPlace ? 4 : 2 * kCpr;                // lanes of a token (of its part that this block moves)
-  constexpr int kRpi = 32 / kL, kU = 4;
-  constexpr int kRound = kThreads / 32 * kRpi * kU;          // tokens of a round
+  constexpr int kRpi = 32 / kL, kIters = kL;                 // tokens of an instruction, instructions of 32 tokens
+  constexpr int kU = kIters < 8 ? kIters : 8;
+  constexpr int kWarps = kThreads / 32;
   const PagedView& a = p.src;
   const PagedView& b = p.dst;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pair = blockIdx.x, seq = pair / a.H, head = pair - seq * a.H;
-  const int chunk = blockIdx.y * kL + lane % kL;
-  const bool is_v = chunk >= kCpr;
-  const int byte = (is_v ? chunk - kCpr : chunk) * 16;
-  const bool scales = a.ks != nullptr && (chunk == 0 || chunk == kCpr);
   pdl_wait_predecessor();
   pdl_allow_successor();
+  const int item = kInPlace ? (int)blockIdx.x : (int)(blockIdx.x * kWarps + warp);
+  const int pair = kInPlace ? item : item / chunks;
+  if (pair >= a.n_seqs * a.H) return;
+  const int seq = pair / a.H, head = pair - seq * a.H;
+  const int chunk = (kInPlace ? (int)blockIdx.y * kL : 0) + lane % kL;
+  const bool is_v = chunk >= kCpr;
+  const int byte = (is_v ? chunk - kCpr : chunk) * 16;
   const int count = __ldcg(p.counts + pair);
   const int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
-  if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) b.lens[seq * b.n_seq + head * b.n_head] = count;
+  const int first = kInPlace ? warp * 32 : (item - pair * chunks) * 32;
+  if (first == 0 && blockIdx.y == 0 && lane == 0) b.lens[seq * b.n_seq + head * b.n_head] = count;
   const int32_t* ta = paged_table(a, seq, head);
   const int32_t* tb = paged_table(b, seq, head);
   const char* from = (is_v ? a.v : a.k) + head * a.head_b + byte;
   char* to = (is_v ? b.v : b.k) + head * b.head_b + byte;
-  for (int j0 = blockIdx.z * kRound; j0 < count; j0 += gridDim.z * kRound) {
-    uint4 x[kU];
-    float sc[kU];
-    int page[kU], row[kU];
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int j = j0 + (u * (kThreads / 32) + warp) * kRpi + lane / kL;
-      page[u] = -1;
-      if (j < count) {
-        const int s = __ldcg(kept + j);
-        if (!(kInPlace && s == j) && s >= 0 && s < a.cap) {
-          int r;
-          const int g = paged_lookup(a, ta, s, r);
-          page[u] = paged_lookup(b, tb, j, row[u]);
-          if (g < 0) page[u] = -1;
-          if (page[u] >= 0) {
-            x[u] = *reinterpret_cast<const uint4*>(from + g * a.page_b + r * a.slot_b);
-            if (scales) sc[u] = (is_v ? a.vs : a.ks)[g * a.sc_page + head * a.sc_head + r * a.sc_slot];
+  const int rounds = kInPlace ? (count + 32 * kWarps - 1) / (32 * kWarps) : (first < count ? 1 : 0);
+  for (int round = 0; round < rounds; ++round) {
+    const int j = round * 32 * kWarps + first + lane;
+    long long src = -1, dst = 0;
+    float sk = 0.f, sv = 0.f;
+    bool scales = false;
+    long long to_scale = 0;
+    if (j < count) {
+      const int s = __ldcg(kept + j);
+      if (!(kInPlace && s == j) && s >= 0 && s < a.cap) {
+        int ra, rb;
+        const int ga = paged_lookup(a, ta, s, ra), gb = paged_lookup(b, tb, j, rb);
+        if (ga >= 0 && gb >= 0) {
+          src = ga * a.page_b + ra * a.slot_b;
+          dst = gb * b.page_b + rb * b.slot_b;
+          if (a.ks && blockIdx.y == 0) {
+            const long long at = ga * a.sc_page + head * a.sc_head + ra * a.sc_slot;
+            to_scale = gb * b.sc_page + head * b.sc_head + rb * b.sc_slot;
+            sk = a.ks[at];
+            sv = a.vs[at];
+            scales = true;
           }
         }
       }
     }
-    if constexpr (kInPlace) __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kU; ++u)
-      if (page[u] >= 0) {
-        *reinterpret_cast<uint4*>(to + page[u] * b.page_b + row[u] * b.slot_b) = x[u];
-        if (scales) (is_v ? b.vs : b.ks)[page[u] * b.sc_page + head * b.sc_head + row[u] * b.sc_slot] = sc[u];
+    for (int i0 = 0; i0 < kIters; i0 += kU) {
+      uint4 x[kU];
+      bool ok[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const long long f = __shfl_sync(0xffffffffu, src, (i0 + u) * kRpi + lane / kL);
+        ok[u] = f >= 0;
+        if (ok[u]) x[u] = *reinterpret_cast<const uint4*>(from + f);
       }
+      if constexpr (kInPlace) __syncthreads();               // kU == kIters: once per round
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const long long t = __shfl_sync(0xffffffffu, dst, (i0 + u) * kRpi + lane / kL);
+        if (ok[u]) *reinterpret_cast<uint4*>(to + t) = x[u];
+      }
+    }
+    if (scales) {
+      b.ks[to_scale] = sk;
+      b.vs[to_scale] = sv;
+    }
   }
 }
 
 // ----------------------------------------------------------------------------- host side
-template <class P>
-cudaError_t launch(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p) {
+template <class P, class... A>
+cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
@@ -476,7 +579,7 @@ cudaError_t launch(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaS
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, more...);
   count_launch();
   return e;
 }
@@ -718,6 +821,7 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
   if (p.dst.n_head == 0 && kv->n_kv_heads > 1 && !(same && p.src.n_head == 0)) return SSD_ERR_INVALID_ARG;
   if (most > p.src.cap) most = p.src.cap;
   if (kept_cols < most || p.dst.cap < most) return SSD_ERR_INVALID_ARG;
+  if ((int64_t)kv->n_seqs * kv->n_kv_heads * ((most + 31) / 32) > 0x7fffffffll) return SSD_ERR_LIMIT;
   if (kv->n_seqs == 0) return SSD_OK;
   p.in_place = into == nullptr;
   p.dst_scores = p.dst.scores != nullptr;
@@ -727,31 +831,18 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
   p.counts = counts;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int pairs = kv->n_seqs * kv->n_kv_heads;
-  // Short rows: 256 threads, so that several heads share an SM.  Long ones: 1024, and up to 48 K keys in shared memory.
-  cudaError_t e;
-  if (p.src.cap <= 8192) {
-    p.keys_cap = p.src.cap;
-    e = launch<EvictParams>(ssd_paged_select_kernel<256>, dim3(pairs), 256, (size_t)p.keys_cap * 4, st, p);
-  } else {
-    p.keys_cap = p.src.cap < 49152 ? p.src.cap : 49152;
-    e = cudaFuncSetAttribute(ssd_paged_select_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, 49152 * 4);
-    if (e == cudaSuccess) e = launch<EvictParams>(ssd_paged_select_kernel<1024>, dim3(pairs), 1024, (size_t)p.keys_cap * 4, st, p);
-  }
+  cudaError_t e = p.src.cap <= 32 * kKeys
+                      ? launch<EvictParams>(ssd_paged_select_short_kernel, dim3((pairs + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, st, p)
+                      : launch<EvictParams>(ssd_paged_select_kernel, dim3(pairs), 1024, 0, st, p);
   if (e == cudaSuccess) {
     const int row = kv->head_dim * elem_bytes(kv->dtype);
-    // elsewhere: enough thread blocks for the whole GPU, each with one round of tokens at least
-    int z = 1;
-    if (into) {
-      const int round = kThreads * 4 / (2 * row / 16);
-      const int rounds = (int)((most + round - 1) / round);
-      z = (int)((148 * 8 + pairs - 1) / pairs);
-      z = z < 1 ? 1 : (z > rounds ? (rounds < 1 ? 1 : rounds) : z);
-    }
-    const dim3 grid(pairs, into ? 1 : 2 * row / 64, z);
+    const int chunks = (int)((most + 31) / 32 > 0 ? (most + 31) / 32 : 1);
+    const long long warps = (long long)pairs * chunks;
+    const dim3 grid = into ? dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))) : dim3(pairs, 2 * row / 64);
     auto* kernel = row == 256 ? (into ? ssd_paged_move_kernel<256, false> : ssd_paged_move_kernel<256, true>)
                               : (row == 128 ? (into ? ssd_paged_move_kernel<128, false> : ssd_paged_move_kernel<128, true>)
                                             : (into ? ssd_paged_move_kernel<64, false> : ssd_paged_move_kernel<64, true>));
-    e = launch<EvictParams>(kernel, grid, kThreads, 0, st, p);
+    e = launch(kernel, grid, kThreads, 0, st, p, chunks);
   }
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;

@@ -109,9 +109,25 @@ __device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, flo
   for (int o = kLanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   scale = __fdiv_rn(m, 448.f);
   const float by = scale > 0.f ? scale : 1.f;
+  // x / by, correctly rounded, from the correctly rounded reciprocal and one remainder (Markstein, IBM J. Res. Dev. 34,
+  // 1990): three operations per value instead of a division.  The theorem leaves out divisors whose significand is all
+  // ones, and wants nothing to overflow or underflow; where it does not hold, divide.
+  const uint32_t bits = __float_as_uint(by);
+  const bool plain = by > 0x1p-100f && by < 0x1p100f && (bits & 0x7fffffu) != 0x7fffffu;
+  const float r = __frcp_rn(by);
+  float q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = x[i] * r;
+    q[i] = fmaf(fmaf(-y, by, x[i]), r, y);
+  }
+  if (!plain) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(x[i], by);
+  }
   uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = paged_e4m3x2(__fdiv_rn(x[2 * i], by), __fdiv_rn(x[2 * i + 1], by));
+  for (int i = 0; i < 4; ++i) c[i] = paged_e4m3x2(q[2 * i], q[2 * i + 1]);
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
 #endif
