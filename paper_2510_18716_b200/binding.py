@@ -531,23 +531,28 @@ class PagedKV:
                               ptr(self._status), p[0], p[1], p[2], s[0], s[1], s[2], t[0], t[1] if len(t) > 1 else 0,
                               n[0], n[1] if len(n) > 1 else 0, w[0], w[1], _PAGED_DTYPES[k_pages.dtype], n_seqs, heads, head_dim,
                               page_size, n_pages, page_table.shape[-1], scores.shape[2] if scores is not None else 0)
-        self._attn = SsdPagedAttn(softmax_scale=float(softmax_scale))
+        self._index = self.device.index
         self._scale = float(softmax_scale)
         self.workspace = workspace
-        self._ready = set()                                  # (n_q_heads, accumulate) that the workspace is known to serve
-        torch.cuda.current_stream(self.device).synchronize() # the status word is zero before another stream's call
-
-    def _check(self, rc, what):
-        if rc != SSD_OK:
-            raise SsdError(rc, what)
+        self._plan = {}                                      # per call: the arguments last checked, and what goes with them
+        self._counts = torch.empty((n_seqs, heads), dtype=torch.int32, device=self.device)
+        home = torch.cuda.current_stream(self.device)
+        self._home = home.cuda_stream
+        home.synchronize()                                   # the status word is zero before another stream's call
 
     def _call(self, fn, *args):
         """fn(*args, stream) with the cache's device current."""
-        index = self.device.index
-        if torch.cuda.current_device() == index:
-            return fn(*args, torch._C._cuda_getCurrentRawStream(index))
-        with torch.cuda.device(index):
-            return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        index = self._index
+        if torch.cuda.current_device() != index:
+            with torch.cuda.device(index):
+                return self._call(fn, *args)
+        stream = torch._C._cuda_getCurrentRawStream(index)
+        if stream != self._home and not torch.cuda.is_current_stream_capturing():
+            # the handle's own memory belongs to the stream that was current when it was made
+            for t in (self.workspace, self._status, self._counts):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream())
+        return fn(*args, stream)
 
     def reserve(self, n_q_heads: int, accumulate: bool = False):
         """Makes the workspace large enough for attention of n_q_heads query heads (with their weights).  The first
@@ -561,8 +566,6 @@ class PagedKV:
                     raise RuntimeError("PagedKV: reserve() the workspace before capturing a graph")
                 self.workspace = torch.zeros(need + 256, dtype=torch.uint8, device=self.device)
                 torch.cuda.current_stream().synchronize()    # zero before any stream uses it
-                self._ready = set()
-        self._ready.add((n_q_heads, bool(accumulate)))
 
     def _rows(self, t: torch.Tensor, heads: int, dtype, what: str):
         if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != dtype or t.device != self.device or t.stride(2) != 1:
@@ -577,21 +580,63 @@ class PagedKV:
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None):
         """Stores the newest tokens, which ``lengths`` already count: k_new, v_new [n_seqs, n_kv_heads, head_dim], one
         per sequence, or [n_tokens, ..] with cu_seqlens int32 [n_seqs + 1] (sequence b's are rows cu[b] .. cu[b+1]-1)."""
-        dtype = self._q_dtype(k_new, "k_new")
-        self._rows(k_new, self.n_kv_heads, dtype, "k_new")
-        self._rows(v_new, self.n_kv_heads, dtype, "v_new")
-        ks, vs = _strides(k_new, 2), _strides(v_new, 2)
-        if k_new.shape != v_new.shape or ks != vs:
-            raise ValueError("PagedKV: k_new and v_new need one shape and the same strides")
-        if cu_seqlens is None:
-            if k_new.shape[0] != self.n_seqs:
+        key = (k_new.shape, k_new.stride(), k_new.dtype, v_new.shape, v_new.stride(), v_new.dtype, cu_seqlens is None)
+        key_was, args = self._plan.get("append", (None, None))
+        if key != key_was:
+            dtype = self._q_dtype(k_new, "k_new")
+            self._rows(k_new, self.n_kv_heads, dtype, "k_new")
+            self._rows(v_new, self.n_kv_heads, dtype, "v_new")
+            ks = _strides(k_new, 2)
+            if k_new.shape != v_new.shape or ks != _strides(v_new, 2):
+                raise ValueError("PagedKV: k_new and v_new need one shape and the same strides")
+            if cu_seqlens is None and k_new.shape[0] != self.n_seqs:
                 raise ValueError(f"PagedKV: {k_new.shape[0]} new rows for {self.n_seqs} sequences, without cu_seqlens")
-        elif cu_seqlens.dtype != torch.int32 or tuple(cu_seqlens.shape) != (self.n_seqs + 1,) or cu_seqlens.device != self.device or cu_seqlens.stride(0) != 1:
+            args = (_PAGED_DTYPES[dtype], ks[0], ks[1], k_new.shape[0])
+            self._plan["append"] = (key, args)
+        self._same_device(k_new, v_new)
+        if cu_seqlens is not None and (cu_seqlens.dtype != torch.int32 or cu_seqlens.shape != (self.n_seqs + 1,) or cu_seqlens.stride(0) != 1
+                                       or cu_seqlens.get_device() != self._index):
             raise ValueError(f"PagedKV: want cu_seqlens int32 [{self.n_seqs + 1}] on {self.device}")
-        self._check(self._call(self.lib.ssd_paged_append, self._kv, k_new.data_ptr(), v_new.data_ptr(), _PAGED_DTYPES[dtype], ks[0], ks[1],
-                               None if cu_seqlens is None else cu_seqlens.data_ptr(), k_new.shape[0]), "ssd_paged_append")
+        rc = self._call(self.lib.ssd_paged_append, self._kv, k_new.data_ptr(), v_new.data_ptr(), args[0], args[1], args[2],
+                        None if cu_seqlens is None else cu_seqlens.data_ptr(), args[3])
+        if rc != SSD_OK:
+            raise SsdError(rc, "ssd_paged_append")
+
+    def _same_device(self, *tensors):
+        for t in tensors:
+            if t.get_device() != self._index:
+                raise ValueError(f"PagedKV: a tensor is on {t.device}, the cache on {self.device}")
 
     def _attend(self, fn, what, q, k_new, v_new, out, return_lse, accumulate):
+        key = (q.shape, q.stride(), q.dtype, return_lse, accumulate)
+        if out is not None:
+            key += (out.shape, out.stride(), out.dtype)
+        if k_new is not None:
+            key += (k_new.shape, k_new.stride(), k_new.dtype, v_new.shape, v_new.stride(), v_new.dtype)
+        plan = self._plan.get(what)
+        if plan is None or plan[0] != key or plan[1] is not self.workspace:
+            plan = self._plan[what] = self._plan_attend(key, q, k_new, v_new, out, bool(return_lse), bool(accumulate))
+        _, _, a, like, lse_like = plan
+        self._same_device(q)
+        if out is None:
+            out = torch.empty_like(q if like is None else like)
+        else:
+            self._same_device(out)
+        a.q, a.out = q.data_ptr(), out.data_ptr()
+        if k_new is not None:
+            self._same_device(k_new, v_new)
+            a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
+        if lse_like is not None:
+            lse = torch.empty_like(lse_like)
+            a.lse = lse.data_ptr()
+        rc = self._call(fn, self._kv, a)
+        if rc != SSD_OK:
+            raise SsdError(rc, what)
+        return out if lse_like is None else (out, lse)
+
+    def _plan_attend(self, key, q, k_new, v_new, out, return_lse, accumulate):
+        """Checks a call's arguments; what a call with the same shapes, strides and types needs besides its pointers:
+        (key, workspace, arguments, a tensor like out if q is not one, a tensor like lse)."""
         dtype = self._q_dtype(q, "q")
         heads = q.shape[1] if q.dim() == 3 else -1
         self._rows(q, heads, dtype, "q")
@@ -599,32 +644,28 @@ class PagedKV:
             raise ValueError(f"PagedKV: q has {q.shape[0]} rows of {heads} heads, the cache {self.n_seqs} of {self.n_kv_heads}")
         if accumulate and self.scores is None:
             raise ValueError("PagedKV: accumulate needs a cache with scores")
+        like = None
         if out is None:
-            out = torch.empty((self.n_seqs, heads, self.head_dim), dtype=dtype, device=self.device)
+            if not q.is_contiguous():
+                like = torch.empty(q.shape, dtype=dtype, device=self.device)
         else:
             self._rows(out, heads, dtype, "out")
             if out.shape[0] != self.n_seqs:
                 raise ValueError(f"PagedKV: out has {out.shape[0]} rows, q {self.n_seqs}")
-        lse = torch.empty((self.n_seqs, heads), dtype=torch.float32, device=self.device) if return_lse else None
-        if (heads, bool(accumulate)) not in self._ready:
-            self.reserve(heads, accumulate)
-        a = self._attn
-        a.q, a.out, a.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        a = SsdPagedAttn(softmax_scale=self._scale, q_dtype=_PAGED_DTYPES[dtype], n_q_heads=heads, accumulate=int(accumulate))
         a.q_seq_stride, a.q_head_stride = _strides(q, 2)
-        a.out_seq_stride, a.out_head_stride = _strides(out, 2)
-        a.q_dtype, a.n_q_heads, a.accumulate = _PAGED_DTYPES[dtype], heads, int(bool(accumulate))
+        a.out_seq_stride, a.out_head_stride = _strides(out if out is not None else (q if like is None else like), 2)
         if k_new is not None:
             self._rows(k_new, self.n_kv_heads, dtype, "k_new")
             self._rows(v_new, self.n_kv_heads, dtype, "v_new")
-            ks, vs = _strides(k_new, 2), _strides(v_new, 2)
-            if k_new.shape[0] != self.n_seqs or k_new.shape != v_new.shape or ks != vs:
+            ks = _strides(k_new, 2)
+            if k_new.shape[0] != self.n_seqs or k_new.shape != v_new.shape or ks != _strides(v_new, 2):
                 raise ValueError(f"PagedKV: want k_new and v_new [{self.n_seqs}, ..] with the same strides")
-            a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
             a.new_seq_stride, a.new_head_stride = ks
+        self.reserve(heads, accumulate)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         a.workspace, a.workspace_bytes = base, self.workspace.numel() - (base - self.workspace.data_ptr())
-        self._check(self._call(fn, self._kv, a), what)
-        return (out, lse) if return_lse else out
+        return key, self.workspace, a, like, torch.empty((self.n_seqs, heads), dtype=torch.float32, device=self.device) if return_lse else None
 
     def decode_attn(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, return_lse: bool = False, accumulate: bool = False):
         """Attention of one new token per sequence, q [n_seqs, n_q_heads, head_dim], over all slots held (zeros where
@@ -645,19 +686,26 @@ class PagedKV:
         n], -1 behind the last one."""
         if self.scores is None:
             raise ValueError("PagedKV: evict needs a cache with scores")
-        h = self.n_kv_heads
-        b = [int(budget)] * h if np.ndim(budget) == 0 else [int(x) for x in budget]
-        r = [int(recent)] * h if np.ndim(recent) == 0 else [int(x) for x in recent]
-        if len(b) != h or len(r) != h or min(b) < 0 or min(r) < 0 or prefix < 0 or prefix + max(map(sum, zip(b, r))) >= 1 << 31:
-            raise ValueError(f"PagedKV: want prefix >= 0, and budget and recent >= 0, one or {h} of them")
-        if into is not None and into.device != self.device:
+        one = (int, np.integer)
+        key = (prefix, budget if isinstance(budget, one) else tuple(budget), recent if isinstance(recent, one) else tuple(recent))
+        plan = self._plan.get("evict")
+        if plan is None or plan[0] != key:
+            h = self.n_kv_heads
+            b = [int(budget)] * h if isinstance(budget, one) else [int(x) for x in budget]
+            r = [int(recent)] * h if isinstance(recent, one) else [int(x) for x in recent]
+            if len(b) != h or len(r) != h or min(b) < 0 or min(r) < 0 or prefix < 0 or prefix + max(map(sum, zip(b, r))) >= 1 << 31:
+                raise ValueError(f"PagedKV: want prefix >= 0, and budget and recent >= 0, one or {h} of them")
+            cols = max(1, min(int(prefix) + max(map(sum, zip(b, r))), self.capacity))
+            ints = C.c_int32 * h
+            plan = self._plan["evict"] = (key, ints(*b), ints(*r), (self.n_seqs, h, cols))
+        if into is not None and into._index != self._index:
             raise ValueError("PagedKV: both caches have to be on one device")
-        cols = max(1, min(int(prefix) + max(map(sum, zip(b, r))), self.capacity))
-        buf = torch.empty(self.n_seqs * h * (cols + 1), dtype=torch.int32, device=self.device)
-        kept = buf[: self.n_seqs * h * cols].view(self.n_seqs, h, cols)
-        ints = C.c_int32 * h
-        self._check(self._call(self.lib.ssd_paged_evict, self._kv, None if into is None else into._kv, int(prefix), ints(*b), ints(*r),
-                               buf.data_ptr(), cols, buf.data_ptr() + 4 * self.n_seqs * h * cols), "ssd_paged_evict")
+        _, b, r, shape = plan
+        kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+        rc = self._call(self.lib.ssd_paged_evict, self._kv, None if into is None else into._kv, int(prefix), b, r, kept.data_ptr(), shape[2],
+                        self._counts.data_ptr())
+        if rc != SSD_OK:
+            raise SsdError(rc, "ssd_paged_evict")
         return kept
 
     def device_status(self) -> int:

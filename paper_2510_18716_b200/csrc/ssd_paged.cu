@@ -273,23 +273,18 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The need-th largest of the keys that the threads of a group (a warp, or a thread block) hold, bit by bit from the top:
-// a bit is set iff at least `need` keys are not below the value with it.  `count(k)`: how many of the group's keys are >= k.
-// Returns the value; whole: exactly `need` keys are at or above it.
+// The need-th largest of the keys that a group of threads holds, bit by bit, from bit `from` - 1 down to bit `to`, t being
+// what the bits above have come to: a bit is set iff at least `need` keys are not below the value with it.  count(k): how many
+// of the group's keys are >= k.  True: exactly `need` keys are at or above t.
 template <class F>
-__device__ __forceinline__ uint32_t nth_key(uint32_t need, F count, bool& whole) {
-  uint32_t t = 0u;
-  whole = false;
+__device__ __forceinline__ bool nth_key(uint32_t need, int from, int to, uint32_t& t, F count) {
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-    const uint32_t n = count(t | bit);
-    if (n >= need) t |= bit;
-    if (n == need) {
-      whole = true;
-      break;
-    }
+  for (int bit = from - 1; bit >= to; --bit) {
+    const uint32_t n = count(t | (1u << bit));
+    if (n >= need) t |= 1u << bit;
+    if (n == need) return true;
   }
-  return t;
+  return false;
 }
 
 // What a (sequence, head) keeps besides the candidates chosen, and the number of them all.
@@ -314,11 +309,6 @@ __device__ __forceinline__ EvictHead evict_head(const EvictParams& p, int pair) 
   e.to = p.dst_scores && !(e.all && p.in_place) ? paged_scores(p.dst, seq, head) : nullptr;
   return e;
 }
-__device__ __forceinline__ float evict_score(const EvictParams& p, const EvictHead& e, int slot) {
-  if (slot < p.src.score_slots) return e.scores[slot];
-  paged_flag(p.src, kPagedBadScores);
-  return 0.f;
-}
 // Everything that is not a choice, by kT threads.
 template <int kT>
 __device__ __forceinline__ void list_rest(const EvictParams& p, const EvictHead& e, int pair, int tid) {
@@ -329,14 +319,15 @@ __device__ __forceinline__ void list_rest(const EvictParams& p, const EvictHead&
     for (int j = tid; j < e.recent; j += kT) e.kept[p.prefix + e.budget + j] = e.n - e.recent + j;
   }
   for (int j = e.count + tid; j < p.kept_cols; j += kT) e.kept[j] = -1;
-  if (tid == 0) p.counts[pair] = e.count;
+  if (tid == 0) {
+    p.counts[pair] = e.count;
+    if (!e.all && e.budget > 0 && e.n - e.recent > p.src.score_slots) paged_flag(p.src, kPagedBadScores);    // candidates without a score: 0
+  }
 }
-// Four rounds of kT scores travel with their tokens at a time, all read before the first is written.  In place that keeps
-// it right: sources lie at or above their destinations, so what is written here is not read by a later round.
-template <int kT, class S>
-__device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHead& e, int tid, S sync) {
-  if (!e.to) return;
-  sync();                                                    // the list is complete
+// Scores travel with their tokens, by all kT threads of a thread block, four rounds at a time, all read before the first is
+// written.  In place that keeps it right: sources lie at or above their destinations, so what is written here is not read later.
+template <int kT>
+__device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHead& e, const int32_t* kept, int tid) {
   for (int j0 = 0; j0 < e.count; j0 += 4 * kT) {
     float x[4];
 #pragma unroll
@@ -344,11 +335,11 @@ __device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHea
       const int j = j0 + u * kT + tid;
       x[u] = 0.f;
       if (j < e.count) {
-        const int s = e.kept[j];
+        const int s = kept[j];
         if (s < p.src.score_slots) x[u] = e.scores[s];
       }
     }
-    if (p.in_place) sync();
+    if (p.in_place) __syncthreads();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int j = j0 + u * kT + tid;
@@ -359,211 +350,259 @@ __device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHea
   }
 }
 
-constexpr int kKeys = 32;                                    // keys of a thread
+constexpr int kShort = 1024;                                 // slots of a short table
 
-// Tables of up to 1024 slots: a warp per (sequence, head), its keys in registers, no barrier.  (Thread blocks of 256
-// threads with histograms of the keys' digits took 19 us for 64 x 32 heads of up to 640 slots, this 7.)
-__global__ void __launch_bounds__(kThreads) ssd_paged_select_short_kernel(const __grid_constant__ EvictParams p) {
-  const int lane = threadIdx.x & 31;
-  const int pair = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  pdl_wait_predecessor();
-  pdl_allow_successor();
-  if (pair >= p.src.n_seqs * p.src.H) return;
-  const EvictHead e = evict_head(p, pair);
-  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
-  const bool choose = !e.all && e.budget > 0;
-  uint32_t key[kKeys];
-  if (choose) {
-#pragma unroll
-    for (int r = 0; r < kKeys; ++r) key[r] = r * 32 + lane < nc ? score_key(evict_score(p, e, p.prefix + r * 32 + lane)) : 0u;
-  }
-  list_rest<32>(p, e, pair, lane);
-  if (choose) {
-    bool whole;
-    // keys that do not exist are 0 and are counted only for k == 0, which is not asked for
-    const uint32_t t = nth_key((uint32_t)e.budget, [&](uint32_t k) {
-      uint32_t n = 0u;
-#pragma unroll
-      for (int r = 0; r < kKeys; ++r) n += key[r] >= k;
-      return __reduce_add_sync(0xffffffffu, n);
-    }, whole);
-    // the keys above t, and the first ones equal to it that make up the budget
-    uint32_t above = 0u;
-#pragma unroll
-    for (int r = 0; r < kKeys; ++r) above += key[r] > t;
-    above = __reduce_add_sync(0xffffffffu, above);
-    uint32_t need = whole ? 0xffffffffu : (uint32_t)e.budget - above;
-    const unsigned below = (1u << lane) - 1u;
-    uint32_t at = 0u;
-#pragma unroll
-    for (int r = 0; r < kKeys; ++r) {
-      const int i = r * 32 + lane;
-      const unsigned equal = __ballot_sync(0xffffffffu, i < nc && key[r] == t);
-      const bool mine = i < nc && (key[r] > t || (key[r] == t && (uint32_t)__popc(equal & below) < need));
-      const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) e.kept[p.prefix + at + __popc(taken & below)] = p.prefix + i;
-      at += __popc(taken);
-      need -= min(need, (uint32_t)__popc(equal));
-    }
-  }
-  move_scores<32>(p, e, lane, [] { __syncwarp(); });
-}
-
-// Longer tables: a thread block per (sequence, head).  Up to 32 K candidates in registers, each warp a run of them; beyond,
-// they are read again for every bit.
-__global__ void __launch_bounds__(1024) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
-  constexpr int kT = 1024, kW = kT / 32;
+// The choice of a (sequence, head) by a thread block of kT threads with up to kK keys each in registers, every warp a run of
+// the candidates; more candidates than that are read again for every bit.  The first kFirst bits look at all keys; those that
+// agree with the result so far are then gathered in `list` (kK * kT values), and the other bits look at them alone.
+// out[k]: the k-th of the chosen candidates, a slot.  The caller's next barrier completes it.
+template <int kT, int kK, int kFirst>
+__device__ __forceinline__ void choose(const EvictParams& p, const EvictHead& e, uint32_t* list, int32_t* out) {
+  constexpr int kW = kT / 32;
   __shared__ uint32_t s_count[2][kW];
-  __shared__ uint32_t s_above[kW], s_equal[kW];
+  __shared__ uint32_t s_above[kW], s_equal[kW], s_len;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int pair = blockIdx.x;
-  pdl_wait_predecessor();
-  pdl_allow_successor();
-  const EvictHead e = evict_head(p, pair);
-  const int nc = e.n - e.recent - p.prefix;
-  if (!e.all && e.budget > 0) {
-    const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;     // candidates of a warp
-    const int a = min(nc, warp * seg), b = min(nc, a + seg), rounds = seg / 32;
-    const bool held = rounds <= kKeys;
-    uint32_t key[kKeys];
-    auto fetch = [&](int r) {
-      const int i = a + r * 32 + lane;
-      return i < b ? score_key(evict_score(p, e, p.prefix + i)) : 0u;
-    };
+  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
+  const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;       // of a warp
+  const int a = min(nc, warp * seg), b = min(nc, a + seg), rounds = seg / 32;
+  const bool held = rounds <= kK;
+  uint32_t key[kK];
+  const int scored = min(b, p.src.score_slots - p.prefix);
+  auto load = [&](int r) { return a + r * 32 + lane < scored ? e.scores[p.prefix + a + r * 32 + lane] : 0.f; };
+  auto fetch = [&](int r) { return a + r * 32 + lane < b ? score_key(load(r)) : 0u; };
+  if (tid == 0) s_len = 0u;
 #pragma unroll
-    for (int r = 0; r < kKeys; ++r) key[r] = held && r < rounds ? fetch(r) : 0u;
-    list_rest<kT>(p, e, pair, tid);
-    auto each = [&](auto f) {                                // f(round, key) for the rounds of this warp, in order
-      if (held) {
+  for (int r = 0; r < kK; ++r) key[r] = held && r < rounds ? __float_as_uint(load(r)) : 0u;            // all loads before the first use
 #pragma unroll
-        for (int r = 0; r < kKeys; ++r)
-          if (r < rounds) f(r, key[r]);
-      } else {
-#pragma unroll 4
-        for (int r = 0; r < rounds; ++r) f(r, fetch(r));
+  for (int r = 0; r < kK; ++r) key[r] = a + r * 32 + lane < b ? score_key(__uint_as_float(key[r])) : 0u;
+  auto each = [&](auto f) {                                  // f(round, key) for the rounds of this warp, in order
+    if (held) {
+#pragma unroll
+      for (int r = 0; r < kK; ++r) {
+        if (kK > 4 && r >= rounds) break;
+        f(r, key[r]);
       }
-    };
-    int turn = 0;
-    bool whole;
-    const uint32_t t = nth_key((uint32_t)e.budget, [&](uint32_t k) {
-      uint32_t n = 0u;
-      each([&](int, uint32_t x) { n += x >= k; });
-      n = __reduce_add_sync(0xffffffffu, n);
-      turn ^= 1;                                             // two sets of counts: one barrier per bit
-      if (lane == 0) s_count[turn][warp] = n;
-      __syncthreads();
-      return __reduce_add_sync(0xffffffffu, s_count[turn][lane]);
-    }, whole);
-    uint32_t above = 0u, equal = 0u;
-    each([&](int r, uint32_t x) {
-      const bool in = a + r * 32 + lane < b;
-      above += in && x > t;
-      equal += in && x == t;
-    });
-    above = __reduce_add_sync(0xffffffffu, above);
-    equal = __reduce_add_sync(0xffffffffu, equal);
-    if (lane == 0) { s_above[warp] = above; s_equal[warp] = equal; }
+    } else {
+#pragma unroll 4
+      for (int r = 0; r < rounds; ++r) f(r, fetch(r));
+    }
+  };
+  int turn = 0;
+  auto sum = [&](uint32_t n) {                               // over the thread block; two sets of counts: one barrier each
+    n = __reduce_add_sync(0xffffffffu, n);
+    turn ^= 1;
+    if (lane == 0) s_count[turn][warp] = n;
     __syncthreads();
-    const uint32_t all_above = __reduce_add_sync(0xffffffffu, s_above[lane]);
-    const uint32_t need = whole ? 0xffffffffu : (uint32_t)e.budget - all_above;              // of the equal ones, the first
-    const uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_equal[lane] : 0u);
-    const uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_above[lane] : 0u);
+    return __reduce_add_sync(0xffffffffu, lane < kW ? s_count[turn][lane] : 0u);
+  };
+  // keys that do not exist are 0 and are counted only for k == 0, which is not asked for
+  const uint32_t budget = (uint32_t)e.budget;
+  uint32_t t = 0u;
+  bool whole = nth_key(budget, 32, 32 - kFirst, t, [&](uint32_t k) {
+    uint32_t n = 0u;
+    each([&](int, uint32_t x) { n += x >= k; });
+    return sum(n);
+  });
+  if (kFirst < 32 && !whole) {
+    constexpr int kRest = 32 - kFirst;
+    const uint32_t top = t >> kRest;
+    uint32_t over = 0u;                                      // keys above all that agree
+    each([&](int r, uint32_t x) {
+      const bool same = a + r * 32 + lane < b && x >> kRest == top;
+      over += x >> kRest > top;
+      const unsigned m = __ballot_sync(0xffffffffu, same);
+      if (m == 0u) return;
+      uint32_t at = 0u;
+      if (lane == 0) at = atomicAdd(&s_len, (uint32_t)__popc(m));
+      at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1u));
+      if (same && at < kK * kT) list[at] = x;
+    });
+    over = sum(over);                                        // a barrier: the list is complete
+    const uint32_t len = s_len;
+    whole = nth_key(budget, kRest, 0, t, [&](uint32_t k) {
+      uint32_t n = 0u;
+      if (len <= kK * kT) {
+        for (uint32_t i = tid; i < len; i += kT) n += list[i] >= k;
+        return sum(n) + over;
+      }
+      each([&](int, uint32_t x) { n += x >= k; });
+      return sum(n);
+    });
+  }
+  // the keys above t, and the first ones equal to it that make up the budget
+  uint32_t above = 0u, equal = 0u;
+  each([&](int r, uint32_t x) {
+    const bool in = a + r * 32 + lane < b;
+    above += in && x > t;
+    equal += in && x == t;
+  });
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = __reduce_add_sync(0xffffffffu, equal);
+  if (lane == 0) { s_above[warp] = above; s_equal[warp] = equal; }
+  __syncthreads();
+  const uint32_t all_above = __reduce_add_sync(0xffffffffu, lane < kW ? s_above[lane] : 0u);
+  const uint32_t all_equal = __reduce_add_sync(0xffffffffu, lane < kW ? s_equal[lane] : 0u);
+  const uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_equal[lane] : 0u);
+  const uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_above[lane] : 0u);
+  const unsigned below = (1u << lane) - 1u;
+  if (all_above + all_equal == budget) {                     // no tie at the border
+    uint32_t at = gt_before + eq_before;
+    each([&](int r, uint32_t x) {
+      const int i = a + r * 32 + lane;
+      const bool mine = i < b && x >= t;
+      const unsigned taken = __ballot_sync(0xffffffffu, mine);
+      if (mine) out[at + __popc(taken & below)] = p.prefix + i;
+      at += __popc(taken);
+    });
+  } else {
+    const uint32_t need = budget - all_above;
     uint32_t at = gt_before + min(eq_before, need), eq = eq_before;
-    const unsigned below = (1u << lane) - 1u;
     each([&](int r, uint32_t x) {
       const int i = a + r * 32 + lane;
       const unsigned same = __ballot_sync(0xffffffffu, i < b && x == t);
       const bool mine = i < b && (x > t || (x == t && eq + __popc(same & below) < need));
       const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) e.kept[p.prefix + at + __popc(taken & below)] = p.prefix + i;
+      if (mine) out[at + __popc(taken & below)] = p.prefix + i;
       at += __popc(taken);
       eq += __popc(same);
     });
-  } else {
-    list_rest<kT>(p, e, pair, tid);
   }
-  move_scores<kT>(p, e, tid, [] { __syncthreads(); });
+}
+
+// Any table: a thread block per (sequence, head) makes the list.  Up to 32 K candidates in registers; the first twelve bits
+// (sign, exponent, three of the mantissa) look at all of them.
+constexpr int kLongThreads = 512, kLongKeys = 64;
+
+__global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
+  extern __shared__ uint32_t s_list[];
+  const int tid = threadIdx.x;
+  const int pair = blockIdx.x;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const EvictHead e = evict_head(p, pair);
+  list_rest<kLongThreads>(p, e, pair, tid);
+  if (!e.all && e.budget > 0) choose<kLongThreads, kLongKeys, 12>(p, e, s_list, e.kept + p.prefix);
+  if (!e.to) return;
+  __syncthreads();                                           // the list is complete
+  move_scores<kLongThreads>(p, e, e.kept, tid);
 }
 
 // ----------------------------------------------------------------------------- eviction: moving the rows
-// Token j of a head comes from slot kept[j] >= j.  A warp moves 32 tokens: each lane looks one of them up (source and
-// destination pages) and copies its scales, then 2 row bytes / 16 lanes at a time copy a token's K and V rows.
-// In place, one thread block has 64 bytes of every row of a head (blockIdx.y), in rounds of 256 tokens: all rows of a round
-// are read before the first is written, and later rounds read only above what it writes.
-template <int kRow, bool kInPlace>
-__global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_constant__ EvictParams p, int chunks) {
-  constexpr int kCpr = kRow / 16;                            // 16-byte chunks of a row; a token has twice as many
-  constexpr int kL = kInPlace ? 4 : 2 * kCpr;                // lanes of a token (of its part that this block moves)
-  constexpr int kRpi = 32 / kL, kIters = kL;                 // tokens of an instruction, instructions of 32 tokens
-  constexpr int kU = kIters < 8 ? kIters : 8;
-  constexpr int kWarps = kThreads / 32;
+// Token j of a head comes from slot kept[j] >= j.  A warp moves kTokens of them: each lane looks one up (source and
+// destination pages) and copies its scales, then kL lanes at a time copy `kL` chunks of 16 bytes of a token, from chunk
+// `chunk0` of its K row and V row side by side.  barrier(): between the last read and the first write of eight instructions.
+template <int kRow, int kL, int kTokens, class B>
+__device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int head, int lane, int chunk0, bool scales, bool in_place, int j0, int count,
+                                            const int32_t* kept, B barrier) {
+  constexpr int kCpr = kRow / 16, kRpi = 32 / kL, kIters = kTokens / kRpi, kU = kIters < 8 ? kIters : 8;
   const PagedView& a = p.src;
   const PagedView& b = p.dst;
+  const int chunk = chunk0 + lane % kL;
+  const bool is_v = chunk >= kCpr;
+  const int byte = (is_v ? chunk - kCpr : chunk) * 16;
+  const char* from = (is_v ? a.v : a.k) + head * a.head_b + byte;
+  char* to = (is_v ? b.v : b.k) + head * b.head_b + byte;
+  const int j = j0 + lane;
+  long long src = -1, dst = 0, to_scale = -1;
+  float sk = 0.f, sv = 0.f;
+  if (lane < kTokens && j < count) {
+    const int s = kept[j];
+    if (!(in_place && s == j) && s >= 0 && s < a.cap) {
+      int ra, rb;
+      const int ga = paged_lookup(a, paged_table(a, seq, head), s, ra), gb = paged_lookup(b, paged_table(b, seq, head), j, rb);
+      if (ga >= 0 && gb >= 0) {
+        src = ga * a.page_b + ra * a.slot_b;
+        dst = gb * b.page_b + rb * b.slot_b;
+        if (scales) {
+          const long long at = ga * a.sc_page + head * a.sc_head + ra * a.sc_slot;
+          to_scale = gb * b.sc_page + head * b.sc_head + rb * b.sc_slot;
+          sk = a.ks[at];
+          sv = a.vs[at];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i0 = 0; i0 < kIters; i0 += kU) {
+    uint4 x[kU];
+    bool ok[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const long long f = __shfl_sync(0xffffffffu, src, (i0 + u) * kRpi + lane / kL);
+      ok[u] = f >= 0;
+      if (ok[u]) x[u] = *reinterpret_cast<const uint4*>(from + f);
+    }
+    barrier();
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const long long t = __shfl_sync(0xffffffffu, dst, (i0 + u) * kRpi + lane / kL);
+      if (ok[u]) *reinterpret_cast<uint4*>(to + t) = x[u];
+    }
+  }
+  if (to_scale >= 0) {
+    b.ks[to_scale] = sk;
+    b.vs[to_scale] = sv;
+  }
+}
+
+// From the list of ssd_paged_select_kernel.  Elsewhere: a warp per 32 tokens.  In place: a thread block has 64 bytes of every
+// row of a head (blockIdx.y), in rounds of 256 tokens: all rows of a round are read before the first is written, and later
+// rounds read only above what it writes.
+template <int kRow, bool kInPlace>
+__global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_constant__ EvictParams p, int chunks) {
+  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait_predecessor();
   pdl_allow_successor();
   const int item = kInPlace ? (int)blockIdx.x : (int)(blockIdx.x * kWarps + warp);
   const int pair = kInPlace ? item : item / chunks;
-  if (pair >= a.n_seqs * a.H) return;
-  const int seq = pair / a.H, head = pair - seq * a.H;
-  const int chunk = (kInPlace ? (int)blockIdx.y * kL : 0) + lane % kL;
-  const bool is_v = chunk >= kCpr;
-  const int byte = (is_v ? chunk - kCpr : chunk) * 16;
+  if (pair >= p.src.n_seqs * p.src.H) return;
+  const int seq = pair / p.src.H, head = pair - seq * p.src.H;
   const int count = __ldcg(p.counts + pair);
   const int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
   const int first = kInPlace ? warp * 32 : (item - pair * chunks) * 32;
-  if (first == 0 && blockIdx.y == 0 && lane == 0) b.lens[seq * b.n_seq + head * b.n_head] = count;
-  const int32_t* ta = paged_table(a, seq, head);
-  const int32_t* tb = paged_table(b, seq, head);
-  const char* from = (is_v ? a.v : a.k) + head * a.head_b + byte;
-  char* to = (is_v ? b.v : b.k) + head * b.head_b + byte;
-  const int rounds = kInPlace ? (count + 32 * kWarps - 1) / (32 * kWarps) : (first < count ? 1 : 0);
-  for (int round = 0; round < rounds; ++round) {
-    const int j = round * 32 * kWarps + first + lane;
-    long long src = -1, dst = 0;
-    float sk = 0.f, sv = 0.f;
-    bool scales = false;
-    long long to_scale = 0;
-    if (j < count) {
-      const int s = __ldcg(kept + j);
-      if (!(kInPlace && s == j) && s >= 0 && s < a.cap) {
-        int ra, rb;
-        const int ga = paged_lookup(a, ta, s, ra), gb = paged_lookup(b, tb, j, rb);
-        if (ga >= 0 && gb >= 0) {
-          src = ga * a.page_b + ra * a.slot_b;
-          dst = gb * b.page_b + rb * b.slot_b;
-          if (a.ks && blockIdx.y == 0) {
-            const long long at = ga * a.sc_page + head * a.sc_head + ra * a.sc_slot;
-            to_scale = gb * b.sc_page + head * b.sc_head + rb * b.sc_slot;
-            sk = a.ks[at];
-            sv = a.vs[at];
-            scales = true;
-          }
-        }
-      }
-    }
-#pragma unroll
-    for (int i0 = 0; i0 < kIters; i0 += kU) {
-      uint4 x[kU];
-      bool ok[kU];
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const long long f = __shfl_sync(0xffffffffu, src, (i0 + u) * kRpi + lane / kL);
-        ok[u] = f >= 0;
-        if (ok[u]) x[u] = *reinterpret_cast<const uint4*>(from + f);
-      }
-      if constexpr (kInPlace) __syncthreads();               // kU == kIters: once per round
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const long long t = __shfl_sync(0xffffffffu, dst, (i0 + u) * kRpi + lane / kL);
-        if (ok[u]) *reinterpret_cast<uint4*>(to + t) = x[u];
-      }
-    }
-    if (scales) {
-      b.ks[to_scale] = sk;
-      b.vs[to_scale] = sv;
-    }
+  if (first == 0 && blockIdx.y == 0 && lane == 0) p.dst.lens[seq * p.dst.n_seq + head * p.dst.n_head] = count;
+  const bool scales = p.src.ks != nullptr && blockIdx.y == 0;
+  if constexpr (kInPlace) {
+    for (int j0 = 0; j0 < count; j0 += 32 * kWarps)
+      move_tokens<kRow, 4, 32>(p, seq, head, lane, (int)blockIdx.y * 4, scales, true, j0 + first, count, kept, [] { __syncthreads(); });
+  } else if (first < count) {
+    move_tokens<kRow, kRow / 8, 32>(p, seq, head, lane, 0, scales, false, first, count, kept, [] {});
   }
+}
+
+// Tables of up to kShort slots: one launch, a thread block per (sequence, head) that chooses and then moves scores and rows.
+// While one thread block chooses, others of the SM move.
+template <int kRow, bool kInPlace>
+__global__ void __launch_bounds__(kThreads) ssd_paged_evict_short_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kWarps = kThreads / 32, kL = kRow / 8, kRpi = 32 / kL;
+  __shared__ int32_t s_kept[kShort];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait_predecessor();
+  pdl_allow_successor();
+  const int pair = blockIdx.x, seq = pair / p.src.H, head = pair - seq * p.src.H;
+  const EvictHead e = evict_head(p, pair);
+  const bool chosen = !e.all && e.budget > 0;
+  for (int j = tid; j < (e.all ? e.n : p.prefix); j += kThreads) s_kept[j] = j;
+  if (!e.all)
+    for (int j = tid; j < e.recent; j += kThreads) s_kept[p.prefix + e.budget + j] = e.n - e.recent + j;
+  if (chosen) choose<kThreads, kShort / kThreads, 32>(p, e, nullptr, s_kept + p.prefix);
+  __syncthreads();                                           // the list is complete, and every warp has read the length
+  if (tid == 0) {
+    p.counts[pair] = e.count;
+    p.dst.lens[seq * p.dst.n_seq + head * p.dst.n_head] = e.count;
+    if (chosen && e.n - e.recent > p.src.score_slots) paged_flag(p.src, kPagedBadScores);    // candidates without a score: 0
+  }
+  // ---- rows (in place: in windows of consecutive tokens, read whole before they are written), then the list and the scores
+  if constexpr (kInPlace) {
+    for (int j0 = 0; j0 < e.count; j0 += kWarps * 8 * kRpi)
+      move_tokens<kRow, kL, 8 * kRpi>(p, seq, head, lane, 0, p.src.ks != nullptr, true, j0 + warp * 8 * kRpi, e.count, s_kept, [] { __syncthreads(); });
+  } else {
+    for (int j0 = warp * 8 * kRpi; j0 < e.count; j0 += kWarps * 8 * kRpi)
+      move_tokens<kRow, kL, 8 * kRpi>(p, seq, head, lane, 0, p.src.ks != nullptr, false, j0, e.count, s_kept, [] {});
+  }
+  for (int j = tid; j < p.kept_cols; j += kThreads) e.kept[j] = j < e.count ? s_kept[j] : -1;
+  if (e.to) move_scores<kThreads>(p, e, s_kept, tid);
 }
 
 // ----------------------------------------------------------------------------- host side
@@ -831,18 +870,26 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
   p.counts = counts;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int pairs = kv->n_seqs * kv->n_kv_heads;
-  cudaError_t e = p.src.cap <= 32 * kKeys
-                      ? launch<EvictParams>(ssd_paged_select_short_kernel, dim3((pairs + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, st, p)
-                      : launch<EvictParams>(ssd_paged_select_kernel, dim3(pairs), 1024, 0, st, p);
-  if (e == cudaSuccess) {
-    const int row = kv->head_dim * elem_bytes(kv->dtype);
-    const int chunks = (int)((most + 31) / 32 > 0 ? (most + 31) / 32 : 1);
-    const long long warps = (long long)pairs * chunks;
-    const dim3 grid = into ? dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))) : dim3(pairs, 2 * row / 64);
-    auto* kernel = row == 256 ? (into ? ssd_paged_move_kernel<256, false> : ssd_paged_move_kernel<256, true>)
-                              : (row == 128 ? (into ? ssd_paged_move_kernel<128, false> : ssd_paged_move_kernel<128, true>)
-                                            : (into ? ssd_paged_move_kernel<64, false> : ssd_paged_move_kernel<64, true>));
-    e = launch(kernel, grid, kThreads, 0, st, p, chunks);
+  const int row = kv->head_dim * elem_bytes(kv->dtype);
+  cudaError_t e;
+  // One launch writes lengths while other heads' thread blocks may still read them: not where they are one and the same.
+  if (p.src.cap <= kShort && (into || p.src.n_head != 0 || kv->n_kv_heads == 1)) {
+    auto* kernel = row == 256 ? (into ? ssd_paged_evict_short_kernel<256, false> : ssd_paged_evict_short_kernel<256, true>)
+                              : (row == 128 ? (into ? ssd_paged_evict_short_kernel<128, false> : ssd_paged_evict_short_kernel<128, true>)
+                                            : (into ? ssd_paged_evict_short_kernel<64, false> : ssd_paged_evict_short_kernel<64, true>));
+    e = launch(kernel, dim3(pairs), kThreads, 0, st, p);
+  } else {
+    constexpr int kList = kLongKeys * kLongThreads * 4;
+    e = cudaFuncSetAttribute(ssd_paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kList);
+    if (e == cudaSuccess) e = launch(ssd_paged_select_kernel, dim3(pairs), kLongThreads, kList, st, p);
+    if (e == cudaSuccess) {
+      const int chunks = (int)((most + 31) / 32 > 0 ? (most + 31) / 32 : 1);
+      const dim3 grid = into ? dim3((unsigned)(((long long)pairs * chunks + kThreads / 32 - 1) / (kThreads / 32))) : dim3(pairs, 2 * row / 64);
+      auto* kernel = row == 256 ? (into ? ssd_paged_move_kernel<256, false> : ssd_paged_move_kernel<256, true>)
+                                : (row == 128 ? (into ? ssd_paged_move_kernel<128, false> : ssd_paged_move_kernel<128, true>)
+                                              : (into ? ssd_paged_move_kernel<64, false> : ssd_paged_move_kernel<64, true>));
+      e = launch(kernel, grid, kThreads, 0, st, p, chunks);
+    }
   }
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;
