@@ -8,6 +8,23 @@ namespace {
 
 constexpr int kThreads = 256;
 
+template <class P, class... A>
+cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, more...);
+  count_launch();
+  return e;
+}
+
 // ----------------------------------------------------------------------------- append
 // A warp takes four heads of one token (8 rows, K and V): 2 D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads
 // before the first store.  Bound by the bytes of the rows for a chunk of prompts, by latency for one decode step.
@@ -352,90 +369,37 @@ __device__ __forceinline__ void move_scores(const EvictParams& p, const EvictHea
 
 constexpr int kShort = 1024;                                 // slots of a short table
 
-// The choice of a (sequence, head) by a thread block of kT threads with up to kK keys each in registers, every warp a run of
-// the candidates; more candidates than that are read again for every bit.  The first kFirst bits look at all keys; those that
-// agree with the result so far are then gathered in `list` (kK * kT values), and the other bits look at them alone.
-// out[k]: the k-th of the chosen candidates, a slot.  The caller's next barrier completes it.
-template <int kT, int kK, int kFirst>
-__device__ __forceinline__ void choose(const EvictParams& p, const EvictHead& e, uint32_t* list, int32_t* out) {
-  constexpr int kW = kT / 32;
-  __shared__ uint32_t s_count[2][kW];
-  __shared__ uint32_t s_above[kW], s_equal[kW], s_len;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
-  const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;       // of a warp
-  const int a = min(nc, warp * seg), b = min(nc, a + seg), rounds = seg / 32;
-  const bool held = rounds <= kK;
-  uint32_t key[kK];
-  const int scored = min(b, p.src.score_slots - p.prefix);
-  auto load = [&](int r) { return a + r * 32 + lane < scored ? e.scores[p.prefix + a + r * 32 + lane] : 0.f; };
-  auto fetch = [&](int r) { return a + r * 32 + lane < b ? score_key(load(r)) : 0u; };
-  if (tid == 0) s_len = 0u;
-#pragma unroll
-  for (int r = 0; r < kK; ++r) key[r] = held && r < rounds ? __float_as_uint(load(r)) : 0u;            // all loads before the first use
-#pragma unroll
-  for (int r = 0; r < kK; ++r) key[r] = a + r * 32 + lane < b ? score_key(__uint_as_float(key[r])) : 0u;
-  auto each = [&](auto f) {                                  // f(round, key) for the rounds of this warp, in order
-    if (held) {
-#pragma unroll
-      for (int r = 0; r < kK; ++r) {
-        if (kK > 4 && r >= rounds) break;
-        f(r, key[r]);
-      }
-    } else {
-#pragma unroll 4
-      for (int r = 0; r < rounds; ++r) f(r, fetch(r));
-    }
-  };
-  int turn = 0;
-  auto sum = [&](uint32_t n) {                               // over the thread block; two sets of counts: one barrier each
+// Sum over a thread block of kT threads, with one barrier: two sets of counts are used in turn.
+template <int kT>
+struct BlockSum {
+  uint32_t (*counts)[kT / 32];                               // [2][kT / 32], shared
+  int turn;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) {
+    const int lane = threadIdx.x & 31;
     n = __reduce_add_sync(0xffffffffu, n);
     turn ^= 1;
-    if (lane == 0) s_count[turn][warp] = n;
+    if (lane == 0) counts[turn][threadIdx.x >> 5] = n;
     __syncthreads();
-    return __reduce_add_sync(0xffffffffu, lane < kW ? s_count[turn][lane] : 0u);
-  };
-  // keys that do not exist are 0 and are counted only for k == 0, which is not asked for
-  const uint32_t budget = (uint32_t)e.budget;
-  uint32_t t = 0u;
-  bool whole = nth_key(budget, 32, 32 - kFirst, t, [&](uint32_t k) {
-    uint32_t n = 0u;
-    each([&](int, uint32_t x) { n += x >= k; });
-    return sum(n);
-  });
-  if (kFirst < 32 && !whole) {
-    constexpr int kRest = 32 - kFirst;
-    const uint32_t top = t >> kRest;
-    uint32_t over = 0u;                                      // keys above all that agree
-    each([&](int r, uint32_t x) {
-      const bool same = a + r * 32 + lane < b && x >> kRest == top;
-      over += x >> kRest > top;
-      const unsigned m = __ballot_sync(0xffffffffu, same);
-      if (m == 0u) return;
-      uint32_t at = 0u;
-      if (lane == 0) at = atomicAdd(&s_len, (uint32_t)__popc(m));
-      at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1u));
-      if (same && at < kK * kT) list[at] = x;
-    });
-    over = sum(over);                                        // a barrier: the list is complete
-    const uint32_t len = s_len;
-    whole = nth_key(budget, kRest, 0, t, [&](uint32_t k) {
-      uint32_t n = 0u;
-      if (len <= kK * kT) {
-        for (uint32_t i = tid; i < len; i += kT) n += list[i] >= k;
-        return sum(n) + over;
-      }
-      each([&](int, uint32_t x) { n += x >= k; });
-      return sum(n);
-    });
+    return __reduce_add_sync(0xffffffffu, lane < kT / 32 ? counts[turn][lane] : 0u);
   }
-  // the keys above t, and the first ones equal to it that make up the budget
+};
+
+// The last step of a choice, in the order of the candidates, every warp a run of `rounds` x 32 of them from a up to b:
+// key(r) is this lane's key of round r.  Taken are the keys above t and the first ones equal to it that make up the budget.
+// out[k]: the k-th of them, a slot.  The caller's next barrier completes it.
+template <int kT, class K>
+__device__ __forceinline__ void emit(uint32_t t, uint32_t budget, int prefix, int a, int b, int rounds, K key, int32_t* out) {
+  constexpr int kW = kT / 32;
+  __shared__ uint32_t s_above[kW], s_equal[kW];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t above = 0u, equal = 0u;
-  each([&](int r, uint32_t x) {
+#pragma unroll 4
+  for (int r = 0; r < rounds; ++r) {
+    const uint32_t x = key(r);
     const bool in = a + r * 32 + lane < b;
     above += in && x > t;
     equal += in && x == t;
-  });
+  }
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) { s_above[warp] = above; s_equal[warp] = equal; }
@@ -447,41 +411,171 @@ __device__ __forceinline__ void choose(const EvictParams& p, const EvictHead& e,
   const unsigned below = (1u << lane) - 1u;
   if (all_above + all_equal == budget) {                     // no tie at the border
     uint32_t at = gt_before + eq_before;
-    each([&](int r, uint32_t x) {
+#pragma unroll 4
+    for (int r = 0; r < rounds; ++r) {
       const int i = a + r * 32 + lane;
-      const bool mine = i < b && x >= t;
+      const bool mine = i < b && key(r) >= t;
       const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) out[at + __popc(taken & below)] = p.prefix + i;
+      if (mine) out[at + __popc(taken & below)] = prefix + i;
       at += __popc(taken);
-    });
+    }
   } else {
     const uint32_t need = budget - all_above;
     uint32_t at = gt_before + min(eq_before, need), eq = eq_before;
-    each([&](int r, uint32_t x) {
+#pragma unroll 4
+    for (int r = 0; r < rounds; ++r) {
       const int i = a + r * 32 + lane;
+      const uint32_t x = key(r);
       const unsigned same = __ballot_sync(0xffffffffu, i < b && x == t);
       const bool mine = i < b && (x > t || (x == t && eq + __popc(same & below) < need));
       const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) out[at + __popc(taken & below)] = p.prefix + i;
+      if (mine) out[at + __popc(taken & below)] = prefix + i;
       at += __popc(taken);
       eq += __popc(same);
-    });
+    }
   }
 }
 
-// Any table: a thread block per (sequence, head) makes the list.  Up to 32 K candidates in registers; the first twelve bits
-// (sign, exponent, three of the mantissa) look at all of them.
-constexpr int kLongThreads = 512, kLongKeys = 64;
+// The choice of a (sequence, head) among at most kT * kK candidates, in registers: the smallest key to be taken bit by bit.
+template <int kT, int kK>
+__device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHead& e, int32_t* out) {
+  constexpr int kW = kT / 32;
+  __shared__ uint32_t s_count[2][kW];
+  __shared__ uint32_t s_key[kT * kK];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
+  const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;       // of a warp
+  const int a = min(nc, warp * seg), b = min(nc, a + seg);
+  const int scored = min(b, p.src.score_slots - p.prefix);
+  uint32_t key[kK];
+  float x[kK];                                               // all loads before the first use
+#pragma unroll
+  for (int r = 0; r < kK; ++r) x[r] = r * 32 < seg && a + r * 32 + lane < scored ? e.scores[p.prefix + a + r * 32 + lane] : 0.f;
+#pragma unroll
+  for (int r = 0; r < kK; ++r) {
+    // keys that do not exist are 0 and are counted only for k == 0, which is not asked for
+    key[r] = r * 32 < seg && a + r * 32 + lane < b ? score_key(x[r]) : 0u;
+    s_key[(warp * kK + r) * 32 + lane] = key[r];             // for this lane's own use below
+  }
+  BlockSum<kT> sum = {s_count, 0};
+  uint32_t t = 0u;
+  nth_key((uint32_t)e.budget, 32, 0, t, [&](uint32_t k) {
+    uint32_t n = 0u;
+#pragma unroll
+    for (int r = 0; r < kK; ++r) n += key[r] >= k;
+    return sum(n);
+  });
+  emit<kT>(t, (uint32_t)e.budget, p.prefix, a, b, seg / 32, [&](int r) { return s_key[(warp * kK + r) * 32 + lane]; }, out);
+}
 
+// The choice among any number of candidates, keys of up to kHeld of them in shared memory (beyond, they are worked out from
+// the scores again every time).  A sample of one key per thread gives two values that the smallest key to be taken lies
+// between, 4 standard deviations of the sample's rank to either side; the keys between them are gathered (up to kList) and
+// searched bit by bit.  Where the sample was wrong, or too many keys lie between (equal ones), all keys are searched.
+constexpr int kLongThreads = 1024, kHeld = 32768, kList = 16384, kMargin = 64;
+
+__device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHead& e, uint32_t* s_key, uint32_t* s_list, int32_t* out) {
+  constexpr int kT = kLongThreads, kW = kT / 32;
+  __shared__ uint32_t s_count[2][kW];
+  __shared__ uint32_t s_warp[kW];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
+  const int scored = min(nc, p.src.score_slots - p.prefix);
+  const bool held = nc <= kHeld;
+  auto fetch = [&](int i) { return score_key(i < scored ? e.scores[p.prefix + i] : 0.f); };
+  if (held) {
+    for (int i0 = 0; i0 < nc; i0 += 8 * kT) {
+      float x[8];                                            // all loads before the first use
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = i0 + u * kT + tid < scored ? e.scores[p.prefix + i0 + u * kT + tid] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * kT + tid < nc) s_key[i0 + u * kT + tid] = score_key(x[u]);
+    }
+  }
+  __syncthreads();
+  auto key_of = [&](int i) { return held ? s_key[i] : fetch(i); };
+  BlockSum<kT> sum = {s_count, 0};
+  const uint32_t budget = (uint32_t)e.budget;
+  uint32_t lo = 0u, hi = 0xffffffffu;                        // keys >= hi are taken, keys < lo are not (no key is 0xffffffff)
+  if (nc > 4 * kT) {
+    const uint32_t mine = key_of((int)((long long)tid * nc / kT));
+    const int rank = (int)((long long)budget * kT / nc);
+    const uint32_t r_hi = (uint32_t)max(rank - kMargin, 0), r_lo = (uint32_t)(rank + kMargin);
+    uint32_t t_hi = 0u, t_lo = 0u;                           // the r_hi-th and r_lo-th largest of the sample, to 20 bits
+#pragma unroll 1
+    for (int bit = 31; bit >= 12; --bit) {
+      const uint32_t k_hi = t_hi | (1u << bit), k_lo = t_lo | (1u << bit);
+      const uint32_t n = sum((mine >= k_hi ? 1u : 0u) + (mine >= k_lo ? 0x10000u : 0u));
+      if ((n & 0xffffu) >= r_hi) t_hi = k_hi;
+      if ((n >> 16) >= r_lo) t_lo = k_lo;
+    }
+    if (r_hi > 0u && t_hi < 0xfffff000u) hi = t_hi + 0x1000u;
+    if (r_lo <= kT) lo = t_lo;
+  }
+  // ---- the keys between, and how many are above
+  uint32_t n_above = 0u, n_in = 0u;
+#pragma unroll 4
+  for (int i = tid; i < nc; i += kT) {
+    const uint32_t x = key_of(i);
+    n_above += x >= hi;
+    n_in += x >= lo && x < hi;
+  }
+  uint32_t above = sum(n_above), len, at;
+  {
+    uint32_t inc = n_in;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, s);
+      if (lane >= s) inc += y;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    const uint32_t y = s_warp[lane];
+    len = __reduce_add_sync(0xffffffffu, y);
+    at = __reduce_add_sync(0xffffffffu, lane < warp ? y : 0u) + inc - n_in;
+  }
+  const bool listed = above < budget && budget <= above + len && len <= kList;
+  uint32_t t = 0u;
+  if (listed) {
+#pragma unroll 4
+    for (int i = tid; i < nc; i += kT) {
+      const uint32_t x = key_of(i);
+      if (x >= lo && x < hi) s_list[at++] = x;
+    }
+    __syncthreads();
+    nth_key(budget - above, 32, 0, t, [&](uint32_t k) {
+      uint32_t n = 0u;
+      for (uint32_t i = tid; i < len; i += kT) n += s_list[i] >= k;
+      return sum(n);
+    });
+    t = max(t, lo);                                          // it may stop early, below keys that are not in the list
+  } else {
+    nth_key(budget, 32, 0, t, [&](uint32_t k) {
+      uint32_t n = 0u;
+#pragma unroll 4
+      for (int i = tid; i < nc; i += kT) n += key_of(i) >= k;
+      return sum(n);
+    });
+  }
+  const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
+  const int a = min(nc, warp * seg), b = min(nc, a + seg);
+  emit<kT>(t, budget, p.prefix, a, b, seg / 32, [&](int r) {
+    const int i = a + r * 32 + lane;
+    return i < b ? key_of(i) : 0u;
+  }, out);
+}
+
+// Any table: a thread block per (sequence, head) makes the list.
 __global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t s_list[];
+  extern __shared__ uint32_t s_dynamic[];                    // kHeld keys, kList keys
   const int tid = threadIdx.x;
   const int pair = blockIdx.x;
   pdl_wait_predecessor();
   pdl_allow_successor();
   const EvictHead e = evict_head(p, pair);
   list_rest<kLongThreads>(p, e, pair, tid);
-  if (!e.all && e.budget > 0) choose<kLongThreads, kLongKeys, 12>(p, e, s_list, e.kept + p.prefix);
+  if (!e.all && e.budget > 0) choose_long(p, e, s_dynamic, s_dynamic + kHeld, e.kept + p.prefix);
   if (!e.to) return;
   __syncthreads();                                           // the list is complete
   move_scores<kLongThreads>(p, e, e.kept, tid);
@@ -571,58 +665,108 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_c
   }
 }
 
-// Tables of up to kShort slots: one launch, a thread block per (sequence, head) that chooses and then moves scores and rows.
-// While one thread block chooses, others of the SM move.
-template <int kRow, bool kInPlace>
-__global__ void __launch_bounds__(kThreads) ssd_paged_evict_short_kernel(const __grid_constant__ EvictParams p) {
-  constexpr int kWarps = kThreads / 32, kL = kRow / 8, kRpi = 32 / kL;
+// Tables of up to kShort slots: one launch, a thread block per (sequence, head) that chooses, looks all its tokens up and then
+// moves rows and scores.  While one thread block chooses, others of the SM move.  In place the rows go in windows of
+// consecutive tokens, each read whole before it is written (sources lie at or above their destinations).
+template <int kRow, bool kInPlace, int kT>
+__global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kWarps = kT / 32, kCpr = kRow / 16, kL = 2 * kCpr, kRpi = 32 / kL, kU = 8;
   __shared__ int32_t s_kept[kShort];
+  __shared__ long long s_src[kShort], s_dst[kShort];         // bytes from the head's first row; source -1: nothing to move
+  const PagedView& a = p.src;
+  const PagedView& b = p.dst;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait_predecessor();
   pdl_allow_successor();
-  const int pair = blockIdx.x, seq = pair / p.src.H, head = pair - seq * p.src.H;
+  const int pair = blockIdx.x, seq = pair / a.H, head = pair - seq * a.H;
   const EvictHead e = evict_head(p, pair);
   const bool chosen = !e.all && e.budget > 0;
-  for (int j = tid; j < (e.all ? e.n : p.prefix); j += kThreads) s_kept[j] = j;
+  for (int j = tid; j < (e.all ? e.n : p.prefix); j += kT) s_kept[j] = j;
   if (!e.all)
-    for (int j = tid; j < e.recent; j += kThreads) s_kept[p.prefix + e.budget + j] = e.n - e.recent + j;
-  if (chosen) choose<kThreads, kShort / kThreads, 32>(p, e, nullptr, s_kept + p.prefix);
+    for (int j = tid; j < e.recent; j += kT) s_kept[p.prefix + e.budget + j] = e.n - e.recent + j;
+  if (chosen) choose_short<kT, kShort / kT>(p, e, s_kept + p.prefix);
   __syncthreads();                                           // the list is complete, and every warp has read the length
   if (tid == 0) {
     p.counts[pair] = e.count;
-    p.dst.lens[seq * p.dst.n_seq + head * p.dst.n_head] = e.count;
-    if (chosen && e.n - e.recent > p.src.score_slots) paged_flag(p.src, kPagedBadScores);    // candidates without a score: 0
+    b.lens[seq * b.n_seq + head * b.n_head] = e.count;
+    if (chosen && e.n - e.recent > a.score_slots) paged_flag(a, kPagedBadScores);    // candidates without a score: 0
   }
-  // ---- rows (in place: in windows of consecutive tokens, read whole before they are written), then the list and the scores
-  if constexpr (kInPlace) {
-    for (int j0 = 0; j0 < e.count; j0 += kWarps * 8 * kRpi)
-      move_tokens<kRow, kL, 8 * kRpi>(p, seq, head, lane, 0, p.src.ks != nullptr, true, j0 + warp * 8 * kRpi, e.count, s_kept, [] { __syncthreads(); });
-  } else {
-    for (int j0 = warp * 8 * kRpi; j0 < e.count; j0 += kWarps * 8 * kRpi)
-      move_tokens<kRow, kL, 8 * kRpi>(p, seq, head, lane, 0, p.src.ks != nullptr, false, j0, e.count, s_kept, [] {});
+  const int32_t* ta = paged_table(a, seq, head);
+  const int32_t* tb = paged_table(b, seq, head);
+  for (int j = tid; j < p.kept_cols; j += kT) {
+    long long src = -1, dst = 0;
+    int s = -1;
+    if (j < e.count) {
+      s = s_kept[j];
+      if (!(kInPlace && s == j)) {
+        int ra, rb;
+        const int ga = paged_lookup(a, ta, s, ra), gb = paged_lookup(b, tb, j, rb);
+        if (ga >= 0 && gb >= 0) {
+          src = ga * a.page_b + ra * a.slot_b;
+          dst = gb * b.page_b + rb * b.slot_b;
+        }
+      }
+      s_src[j] = src;
+      s_dst[j] = dst;
+    }
+    e.kept[j] = s;
   }
-  for (int j = tid; j < p.kept_cols; j += kThreads) e.kept[j] = j < e.count ? s_kept[j] : -1;
-  if (e.to) move_scores<kThreads>(p, e, s_kept, tid);
+  __syncthreads();
+  const int chunk = lane % kL;
+  const bool is_v = chunk >= kCpr;
+  const char* from = (is_v ? a.v : a.k) + head * a.head_b + (is_v ? chunk - kCpr : chunk) * 16;
+  char* to = (is_v ? b.v : b.k) + head * b.head_b + (is_v ? chunk - kCpr : chunk) * 16;
+  for (int j0 = 0; j0 < e.count; j0 += kWarps * kU * kRpi) {
+    const int j1 = j0 + warp * kU * kRpi + lane / kL;
+    uint4 x[kU];
+    long long src[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = j1 + u * kRpi;
+      src[u] = j < e.count ? s_src[j] : -1;
+      if (src[u] >= 0) x[u] = *reinterpret_cast<const uint4*>(from + src[u]);
+    }
+    if constexpr (kInPlace) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (src[u] >= 0) *reinterpret_cast<uint4*>(to + s_dst[j1 + u * kRpi]) = x[u];
+  }
+  if (a.ks) {                                                // the scales, like the scores, in rounds of four
+    for (int j0 = 0; j0 < e.count; j0 += 4 * kT) {
+      float sk[4], sv[4];
+      long long put[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = j0 + u * kT + tid;
+        put[u] = -1;
+        if (j < e.count && s_src[j] >= 0) {
+          int ra, rb;
+          const int ga = paged_lookup(a, ta, s_kept[j], ra), gb = paged_lookup(b, tb, j, rb);
+          const long long at = ga * a.sc_page + head * a.sc_head + ra * a.sc_slot;
+          put[u] = gb * b.sc_page + head * b.sc_head + rb * b.sc_slot;
+          sk[u] = a.ks[at];
+          sv[u] = a.vs[at];
+        }
+      }
+      if constexpr (kInPlace) __syncthreads();
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (put[u] >= 0) {
+          b.ks[put[u]] = sk[u];
+          b.vs[put[u]] = sv[u];
+        }
+    }
+  }
+  if (e.to) move_scores<kT>(p, e, s_kept, tid);
+}
+
+template <int kRow, int kT>
+cudaError_t launch_evict_short(const EvictParams& p, int pairs, bool in_place, cudaStream_t st) {
+  return in_place ? launch(ssd_paged_evict_short_kernel<kRow, true, kT>, dim3(pairs), kT, 0, st, p)
+                  : launch(ssd_paged_evict_short_kernel<kRow, false, kT>, dim3(pairs), kT, 0, st, p);
 }
 
 // ----------------------------------------------------------------------------- host side
-template <class P, class... A>
-cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, more...);
-  count_launch();
-  return e;
-}
-
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 int elem_bytes(int dtype) { return dtype == SSD_PAGED_E4M3 ? 1 : 2; }
@@ -874,14 +1018,15 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
   cudaError_t e;
   // One launch writes lengths while other heads' thread blocks may still read them: not where they are one and the same.
   if (p.src.cap <= kShort && (into || p.src.n_head != 0 || kv->n_kv_heads == 1)) {
-    auto* kernel = row == 256 ? (into ? ssd_paged_evict_short_kernel<256, false> : ssd_paged_evict_short_kernel<256, true>)
-                              : (row == 128 ? (into ? ssd_paged_evict_short_kernel<128, false> : ssd_paged_evict_short_kernel<128, true>)
-                                            : (into ? ssd_paged_evict_short_kernel<64, false> : ssd_paged_evict_short_kernel<64, true>));
-    e = launch(kernel, dim3(pairs), kThreads, 0, st, p);
+    // many heads: thread blocks of 128 threads, more of them on an SM; few: of 256, each done sooner
+    const bool many = pairs > 1024;
+    e = row == 256 ? (many ? launch_evict_short<256, 128>(p, pairs, !into, st) : launch_evict_short<256, 256>(p, pairs, !into, st))
+                   : (row == 128 ? (many ? launch_evict_short<128, 128>(p, pairs, !into, st) : launch_evict_short<128, 256>(p, pairs, !into, st))
+                                 : (many ? launch_evict_short<64, 128>(p, pairs, !into, st) : launch_evict_short<64, 256>(p, pairs, !into, st)));
   } else {
-    constexpr int kList = kLongKeys * kLongThreads * 4;
-    e = cudaFuncSetAttribute(ssd_paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kList);
-    if (e == cudaSuccess) e = launch(ssd_paged_select_kernel, dim3(pairs), kLongThreads, kList, st, p);
+    constexpr int kBytes = (kHeld + kList) * 4;
+    e = cudaFuncSetAttribute(ssd_paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e == cudaSuccess) e = launch(ssd_paged_select_kernel, dim3(pairs), kLongThreads, kBytes, st, p);
     if (e == cudaSuccess) {
       const int chunks = (int)((most + 31) / 32 > 0 ? (most + 31) / 32 : 1);
       const dim3 grid = into ? dim3((unsigned)(((long long)pairs * chunks + kThreads / 32 - 1) / (kThreads / 32))) : dim3(pairs, 2 * row / 64);
