@@ -384,16 +384,36 @@ struct BlockSum {
   }
 };
 
-// The last step of a choice, in the order of the candidates, every warp a run of `rounds` x 32 of them from a up to b:
-// key(r) is this lane's key of round r.  Taken are the keys above t and the first ones equal to it that make up the budget.
-// out[k]: the k-th of them, a slot.  The caller's next barrier completes it.
+// The last step of a choice, in the order of the candidates, every warp a run of `rounds` x 32 of them: key(r) is this lane's
+// key of round r, 0 where there is none; a: the run's first candidate, b: the end of them.  Taken are the keys above t and
+// the first ones equal to it that make up the budget.  out[k]: the k-th of them, a slot.  The caller's next barrier
+// completes it.
 template <int kT, class K>
 __device__ __forceinline__ void emit(uint32_t t, uint32_t budget, int prefix, int a, int b, int rounds, K key, int32_t* out) {
   constexpr int kW = kT / 32;
-  __shared__ uint32_t s_above[kW], s_equal[kW];
+  __shared__ uint32_t s_from[kW], s_above[kW];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t n = 0u;
+#pragma unroll 8
+  for (int r = 0; r < rounds; ++r) n += key(r) >= t;
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (lane == 0) s_from[warp] = n;
+  __syncthreads();
+  const uint32_t all = __reduce_add_sync(0xffffffffu, lane < kW ? s_from[lane] : 0u);
+  const uint32_t from_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_from[lane] : 0u);
+  const unsigned below = (1u << lane) - 1u;
+  if (all == budget && t > 0u) {                             // no tie at the border
+    uint32_t at = from_before;
+#pragma unroll 8
+    for (int r = 0; r < rounds; ++r) {
+      const bool mine = key(r) >= t;
+      const unsigned taken = __ballot_sync(0xffffffffu, mine);
+      if (mine) out[at + __popc(taken & below)] = prefix + a + r * 32 + lane;
+      at += __popc(taken);
+    }
+    return;
+  }
   uint32_t above = 0u, equal = 0u;
-#pragma unroll 4
   for (int r = 0; r < rounds; ++r) {
     const uint32_t x = key(r);
     const bool in = a + r * 32 + lane < b;
@@ -402,37 +422,21 @@ __device__ __forceinline__ void emit(uint32_t t, uint32_t budget, int prefix, in
   }
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
-  if (lane == 0) { s_above[warp] = above; s_equal[warp] = equal; }
   __syncthreads();
-  const uint32_t all_above = __reduce_add_sync(0xffffffffu, lane < kW ? s_above[lane] : 0u);
-  const uint32_t all_equal = __reduce_add_sync(0xffffffffu, lane < kW ? s_equal[lane] : 0u);
-  const uint32_t eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_equal[lane] : 0u);
-  const uint32_t gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_above[lane] : 0u);
-  const unsigned below = (1u << lane) - 1u;
-  if (all_above + all_equal == budget) {                     // no tie at the border
-    uint32_t at = gt_before + eq_before;
-#pragma unroll 4
-    for (int r = 0; r < rounds; ++r) {
-      const int i = a + r * 32 + lane;
-      const bool mine = i < b && key(r) >= t;
-      const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) out[at + __popc(taken & below)] = prefix + i;
-      at += __popc(taken);
-    }
-  } else {
-    const uint32_t need = budget - all_above;
-    uint32_t at = gt_before + min(eq_before, need), eq = eq_before;
-#pragma unroll 4
-    for (int r = 0; r < rounds; ++r) {
-      const int i = a + r * 32 + lane;
-      const uint32_t x = key(r);
-      const unsigned same = __ballot_sync(0xffffffffu, i < b && x == t);
-      const bool mine = i < b && (x > t || (x == t && eq + __popc(same & below) < need));
-      const unsigned taken = __ballot_sync(0xffffffffu, mine);
-      if (mine) out[at + __popc(taken & below)] = prefix + i;
-      at += __popc(taken);
-      eq += __popc(same);
-    }
+  if (lane == 0) { s_above[warp] = above; s_from[warp] = equal; }
+  __syncthreads();
+  const uint32_t need = budget - __reduce_add_sync(0xffffffffu, lane < kW ? s_above[lane] : 0u);
+  uint32_t eq = __reduce_add_sync(0xffffffffu, lane < warp ? s_from[lane] : 0u);
+  uint32_t at = __reduce_add_sync(0xffffffffu, lane < warp ? s_above[lane] : 0u) + min(eq, need);
+  for (int r = 0; r < rounds; ++r) {
+    const int i = a + r * 32 + lane;
+    const uint32_t x = key(r);
+    const unsigned same = __ballot_sync(0xffffffffu, i < b && x == t);
+    const bool mine = i < b && (x > t || (x == t && eq + __popc(same & below) < need));
+    const unsigned taken = __ballot_sync(0xffffffffu, mine);
+    if (mine) out[at + __popc(taken & below)] = prefix + i;
+    at += __popc(taken);
+    eq += __popc(same);
   }
 }
 
@@ -469,61 +473,68 @@ __device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHe
 }
 
 // The choice among any number of candidates, keys of up to kHeld of them in shared memory (beyond, they are worked out from
-// the scores again every time).  A sample of one key per thread gives two values that the smallest key to be taken lies
-// between, 4 standard deviations of the sample's rank to either side; the keys between them are gathered (up to kList) and
-// searched bit by bit.  Where the sample was wrong, or too many keys lie between (equal ones), all keys are searched.
-constexpr int kLongThreads = 1024, kHeld = 32768, kList = 16384, kMargin = 64;
+// the scores again every time).  Counts of the keys in 2048 equal bins from the least to the greatest say which bin holds the
+// smallest key to be taken; a bin of few keys is ranked outright, one of many is divided again (at most twice, since 33 bits
+// make three times 11).  A bit at a time, like the short tables, took 44 us for 32768 slots: every step waits for the whole
+// thread block.
+constexpr int kLongThreads = 1024, kHeld = 32768, kBins = 2048, kFew = 256;
 
-__device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHead& e, uint32_t* s_key, uint32_t* s_list, int32_t* out) {
+__device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHead& e, uint32_t* s_key, uint32_t* s_bin, int32_t* out) {
   constexpr int kT = kLongThreads, kW = kT / 32;
-  __shared__ uint32_t s_count[2][kW];
-  __shared__ uint32_t s_warp[kW];
+  static_assert(kBins == 2 * kT, "two bins a thread");
+  __shared__ uint32_t s_min[kW], s_max[kW], s_warp[kW], s_few[kFew];
+  __shared__ uint32_t s_at, s_need, s_in, s_len, s_t;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
   const int scored = min(nc, p.src.score_slots - p.prefix);
   const bool held = nc <= kHeld;
   auto fetch = [&](int i) { return score_key(i < scored ? e.scores[p.prefix + i] : 0.f); };
+  uint32_t lo = 0xffffffffu, hi = 0u;
   if (held) {
-    for (int i0 = 0; i0 < nc; i0 += 8 * kT) {
-      float x[8];                                            // all loads before the first use
+    for (int i0 = 0; i0 < nc; i0 += 16 * kT) {
+      float x[16];                                           // all loads before the first use
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = i0 + u * kT + tid < scored ? e.scores[p.prefix + i0 + u * kT + tid] : 0.f;
+      for (int u = 0; u < 16; ++u) x[u] = i0 + u * kT + tid < scored ? e.scores[p.prefix + i0 + u * kT + tid] : 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (i0 + u * kT + tid < nc) s_key[i0 + u * kT + tid] = score_key(x[u]);
+      for (int u = 0; u < 16; ++u)
+        if (i0 + u * kT + tid < nc) {
+          const uint32_t k = score_key(x[u]);
+          s_key[i0 + u * kT + tid] = k;
+          lo = min(lo, k);
+          hi = max(hi, k);
+        }
+    }
+  } else {
+#pragma unroll 8
+    for (int i = tid; i < nc; i += kT) {
+      const uint32_t k = fetch(i);
+      lo = min(lo, k);
+      hi = max(hi, k);
     }
   }
-  __syncthreads();
   auto key_of = [&](int i) { return held ? s_key[i] : fetch(i); };
-  BlockSum<kT> sum = {s_count, 0};
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) { s_min[warp] = lo; s_max[warp] = hi; }
+  __syncthreads();
+  lo = __reduce_min_sync(0xffffffffu, s_min[lane]);
+  hi = __reduce_max_sync(0xffffffffu, s_max[lane]);
   const uint32_t budget = (uint32_t)e.budget;
-  uint32_t lo = 0u, hi = 0xffffffffu;                        // keys >= hi are taken, keys < lo are not (no key is 0xffffffff)
-  if (nc > 4 * kT) {
-    const uint32_t mine = key_of((int)((long long)tid * nc / kT));
-    const int rank = (int)((long long)budget * kT / nc);
-    const uint32_t r_hi = (uint32_t)max(rank - kMargin, 0), r_lo = (uint32_t)(rank + kMargin);
-    uint32_t t_hi = 0u, t_lo = 0u;                           // the r_hi-th and r_lo-th largest of the sample, to 20 bits
-#pragma unroll 1
-    for (int bit = 31; bit >= 12; --bit) {
-      const uint32_t k_hi = t_hi | (1u << bit), k_lo = t_lo | (1u << bit);
-      const uint32_t n = sum((mine >= k_hi ? 1u : 0u) + (mine >= k_lo ? 0x10000u : 0u));
-      if ((n & 0xffffu) >= r_hi) t_hi = k_hi;
-      if ((n >> 16) >= r_lo) t_lo = k_lo;
+  uint32_t need = budget, t = lo;                            // of the keys from lo to hi; those above hi are taken
+  for (;;) {
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
+    s_bin[tid] = 0u;
+    s_bin[tid + kT] = 0u;
+    if (tid == 0) s_len = 0u;
+    __syncthreads();
+#pragma unroll 8
+    for (int i = tid; i < nc; i += kT) {
+      const uint32_t x = key_of(i);
+      if (x >= lo && x <= hi) atomicAdd(s_bin + ((x - lo) >> shift), 1u);
     }
-    if (r_hi > 0u && t_hi < 0xfffff000u) hi = t_hi + 0x1000u;
-    if (r_lo <= kT) lo = t_lo;
-  }
-  // ---- the keys between, and how many are above
-  uint32_t n_above = 0u, n_in = 0u;
-#pragma unroll 4
-  for (int i = tid; i < nc; i += kT) {
-    const uint32_t x = key_of(i);
-    n_above += x >= hi;
-    n_in += x >= lo && x < hi;
-  }
-  uint32_t above = sum(n_above), len, at;
-  {
-    uint32_t inc = n_in;
+    __syncthreads();
+    const uint32_t c1 = s_bin[kBins - 1 - 2 * tid], c0 = s_bin[kBins - 2 - 2 * tid];         // from the top
+    uint32_t inc = c1 + c0;
 #pragma unroll
     for (int s = 1; s < 32; s <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, inc, s);
@@ -531,32 +542,45 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
     }
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
-    const uint32_t y = s_warp[lane];
-    len = __reduce_add_sync(0xffffffffu, y);
-    at = __reduce_add_sync(0xffffffffu, lane < warp ? y : 0u) + inc - n_in;
-  }
-  const bool listed = above < budget && budget <= above + len && len <= kList;
-  uint32_t t = 0u;
-  if (listed) {
-#pragma unroll 4
-    for (int i = tid; i < nc; i += kT) {
-      const uint32_t x = key_of(i);
-      if (x >= lo && x < hi) s_list[at++] = x;
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u) + inc - c1 - c0;
+    if (before < need && need <= before + c1) {
+      s_at = kBins - 1 - 2 * tid;
+      s_need = need - before;
+      s_in = c1;
+    } else if (before + c1 < need && need <= before + c1 + c0) {
+      s_at = kBins - 2 - 2 * tid;
+      s_need = need - before - c1;
+      s_in = c0;
     }
     __syncthreads();
-    nth_key(budget - above, 32, 0, t, [&](uint32_t k) {
-      uint32_t n = 0u;
-      for (uint32_t i = tid; i < len; i += kT) n += s_list[i] >= k;
-      return sum(n);
-    });
-    t = max(t, lo);                                          // it may stop early, below keys that are not in the list
-  } else {
-    nth_key(budget, 32, 0, t, [&](uint32_t k) {
-      uint32_t n = 0u;
-#pragma unroll 4
-      for (int i = tid; i < nc; i += kT) n += key_of(i) >= k;
-      return sum(n);
-    });
+    need = s_need;
+    const uint32_t in = s_in;
+    lo += s_at << shift;
+    hi = min(hi, lo + ((1u << shift) - 1u));
+    t = lo;
+    if (shift == 0 || need == in) break;                     // equal keys, or the whole bin
+    if (in <= kFew) {
+#pragma unroll 8
+      for (int i = tid; i < nc; i += kT) {
+        const uint32_t x = key_of(i);
+        if (x >= lo && x <= hi) s_few[atomicAdd(&s_len, 1u)] = x;
+      }
+      __syncthreads();
+      // the need-th largest: as many as need - 1 are above it, or need - 1 lies among its equals
+      if (tid < (int)in) {
+        const uint32_t x = s_few[tid];
+        uint32_t above = 0u, from = 0u;
+        for (uint32_t i = 0; i < in; ++i) {
+          const uint32_t y = s_few[i];
+          above += y > x;
+          from += y >= x;
+        }
+        if (above < need && need <= from) s_t = x;           // its equals write the same
+      }
+      __syncthreads();
+      t = s_t;
+      break;
+    }
   }
   const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
   const int a = min(nc, warp * seg), b = min(nc, a + seg);
@@ -568,7 +592,7 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
 
 // Any table: a thread block per (sequence, head) makes the list.
 __global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t s_dynamic[];                    // kHeld keys, kList keys
+  extern __shared__ uint32_t s_dynamic[];                    // kHeld keys, kBins counts
   const int tid = threadIdx.x;
   const int pair = blockIdx.x;
   pdl_wait_predecessor();
@@ -1024,7 +1048,7 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
                    : (row == 128 ? (many ? launch_evict_short<128, 128>(p, pairs, !into, st) : launch_evict_short<128, 256>(p, pairs, !into, st))
                                  : (many ? launch_evict_short<64, 128>(p, pairs, !into, st) : launch_evict_short<64, 256>(p, pairs, !into, st)));
   } else {
-    constexpr int kBytes = (kHeld + kList) * 4;
+    constexpr int kBytes = (kHeld + kBins) * 4;
     e = cudaFuncSetAttribute(ssd_paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e == cudaSuccess) e = launch(ssd_paged_select_kernel, dim3(pairs), kLongThreads, kBytes, st, p);
     if (e == cudaSuccess) {
