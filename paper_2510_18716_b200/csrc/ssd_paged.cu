@@ -107,7 +107,8 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
 
 // ----------------------------------------------------------------------------- joining pieces, and the weights
 // After an attention launch that shared tiles out by warps: the pieces of every head that a share's border has cut are
-// joined, in the order of the workers: by a warp per query head, or by all eight of a thread block where there are many.
+// joined, in the order of the workers: by a warp per query head, or by all eight of a thread block where there are many
+// pieces, or few query heads.
 // Where the weights are wanted, further thread blocks add them to the scores meanwhile:
 //   scores += sum over the query heads of a key head of 2^(logit - m) / l,
 // from the logits that the attention launch left (4 bytes per query head and slot, against 2 row bytes of K and V there),
@@ -121,14 +122,15 @@ __device__ __forceinline__ const float* piece_of(const PagedDecodeParams& p, int
 }
 
 template <int D>
-__device__ void join_heads(const PagedDecodeParams& p, int units, int join_blocks) {
+__device__ void join_heads(const PagedDecodeParams& p, int units, int join_blocks, bool one_each) {
   __shared__ int2 s_pc[kJoinWarps];
   __shared__ float4 s_o[kJoinWarps][D / 4];
   __shared__ float s_m[kJoinWarps], s_l[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int floats = paged_part_floats(p.rows, D);
   // heads that are cut into many pieces tend to be neighbours: the units of a thread block lie far apart
-  auto unit_of = [&](int w) { return w * (int)join_blocks + (int)blockIdx.x; };
+  auto unit_of = [&](int w) { return w * join_blocks + (int)blockIdx.x; };
+  const int alone = one_each ? 1 : kAlone;
   auto of = [&](int unit, int& h, long long& at, char*& out) {        // a query head: its row in a state, and its place
     const int vp = unit / p.rows;
     h = unit - vp * p.rows;
@@ -150,7 +152,7 @@ __device__ void join_heads(const PagedDecodeParams& p, int units, int join_block
   int h = 0;
   int2 pc = make_int2(0, 0);
   const int mine = unit_of(warp);
-  if (mine < units) {
+  if (mine < units && (warp == 0 || !one_each)) {
     long long at;
     char* out;
     if (of(mine, h, at, out)) pc = __ldcg(p.pieces + mine / p.rows);
@@ -158,14 +160,14 @@ __device__ void join_heads(const PagedDecodeParams& p, int units, int join_block
   if (lane == 0) s_pc[warp] = pc;
   float4 o;
   float m, l;
-  if (pc.y > 1 && pc.y <= kAlone) {
+  if (pc.y > 1 && pc.y <= alone) {
     paged_merge<D>(p, lane, h, pc.y, [&](int i) { return piece_of(p, floats, pc.x, i); }, o, m, l);
     finish(mine, o, m, l);
   }
   __syncthreads();
   for (int u = 0; u < kJoinWarps; ++u) {
     const int2 q = s_pc[u];
-    if (q.y <= kAlone) continue;
+    if (q.y <= alone) continue;
     const int hu = unit_of(u) % p.rows;
     const int n = (q.y - warp + kJoinWarps - 1) / kJoinWarps;
     paged_merge<D>(p, lane, hu, n, [&](int i) { return piece_of(p, floats, q.x, i * kJoinWarps + warp); }, o, m, l);
@@ -264,13 +266,14 @@ __device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_pe
 struct JoinParams {
   PagedDecodeParams d;
   int join_blocks, units, blocks_per_pair;   // the thread blocks after the first join_blocks add weights
+  int one_each;                              // a query head per thread block, instead of one per warp
 };
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) ssd_paged_join_kernel(const __grid_constant__ JoinParams p) {
   pdl_wait_predecessor();
   pdl_allow_successor();
-  if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units, p.join_blocks);
+  if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units, p.join_blocks, p.one_each != 0);
   else add_weights(p.d, blockIdx.x - p.join_blocks, p.blocks_per_pair, D, p.join_blocks > 0);
 }
 
@@ -870,7 +873,7 @@ Workspace workspace_of(const PagedView& v, int head_dim, int g, bool accumulate,
   const int rows = paged_rows(g);
   const size_t heads = (size_t)v.n_seqs * v.H * g;
   Workspace w;
-  w.partial = align_up((size_t)sms * 4);
+  w.partial = align_up(paged_max_workers(sms) * 4);
   w.pieces = align_up(w.partial + paged_max_workers(sms) * 2 * paged_part_floats(rows, head_dim) * 4);
   w.ml = align_up(w.pieces + (size_t)v.n_seqs * v.H * ((g + rows - 1) / rows) * 8);
   w.logits = align_up(w.ml + (accumulate ? heads * 8 : 0));
@@ -933,14 +936,21 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   const float scale = a->softmax_scale > 0.f ? a->softmax_scale : 1.f / std::sqrt((float)kv->head_dim);
   p.scale_log2 = scale * 1.44269504088896340736f;
   p.bf16 = a->q_dtype == SSD_PAGED_BF16;
+  // Pieces that one head may be cut into, times query heads: up to 16 a warp joins as it goes (128: a thread block); more
+  // are worth a launch of their own, which spreads them over the GPU (16 query heads x 37 pieces: 62 us against 57 ..).
+  const int row_b = kv->head_dim * elem_bytes(kv->dtype), tiles = (int)((p.c.cap * (long long)row_b + 4095) / 4096);
+  const int heads = p.c.n_seqs * p.c.H * p.qt;
+  const bool many = paged_many(p, sms);
+  const int cuts = many ? (int)(paged_max_workers(sms) / heads) : (sms / heads < (tiles + 7) / 8 ? sms / heads : (tiles + 7) / 8);
+  p.join_later = cuts * p.rows > (many ? 16 : 128);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = kv->dtype == SSD_PAGED_E4M3 ? launch_paged_decode_8(p, kv->head_dim, sms, st) : launch_paged_decode_16(p, kv->head_dim, sms, st);
-  const bool many = paged_many(p, sms);
-  if (e == cudaSuccess && (many || a->accumulate)) {
+  if (e == cudaSuccess && (p.join_later || a->accumulate)) {
     JoinParams j = {};
     j.d = p;
     j.units = p.c.n_seqs * p.c.H * p.qt * p.rows;
-    j.join_blocks = many ? (j.units + kJoinWarps - 1) / kJoinWarps : 0;
+    j.one_each = j.units <= 4 * sms;
+    j.join_blocks = p.join_later ? (j.one_each ? j.units : (j.units + kJoinWarps - 1) / kJoinWarps) : 0;
     j.blocks_per_pair = (p.c.cap + kWeightSlots - 1) / kWeightSlots;
     const int blocks = j.join_blocks + (a->accumulate ? p.c.n_seqs * p.c.H * j.blocks_per_pair : 0);
     e = launch<JoinParams>(kv->head_dim == 128 ? ssd_paged_join_kernel<128> : ssd_paged_join_kernel<64>, dim3((unsigned)blocks), kThreads, 0, st, j);

@@ -161,12 +161,13 @@ struct PagedDecodeParams {
   float* logits;            // weights wanted: [n_seqs * H * g, logit_row]; else null
   float2* ml;               // weights wanted: [n_seqs * H * g] (max, sum)
   long long logit_row;
-  uint32_t* counters;       // [thread blocks] pieces done (few heads), zero between launches
-  int2* pieces;             // [n_seqs * H * qt]: the first worker that has a piece of the head, and how many have (many heads)
+  uint32_t* counters;       // [workers] pieces done, zero between launches
+  int2* pieces;             // [n_seqs * H * qt], join_later only: the first worker that has a piece of the head, and how many have
   float* partial;           // [workers][2][paged_part_floats(rows, D)]
   float scale_log2;
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together
   FastDiv by_qt, by_heads;  // n / qt, n / H
+  int join_later;           // 1: ssd_paged_join_kernel joins the pieces
   int whole_tiles;          // the page size is a multiple of the tile's slots
   int bf16;                 // type of q, out, k_new, v_new: 1 bf16, 0 fp16
 };
@@ -182,8 +183,8 @@ __host__ __device__
 #endif
 inline int paged_part_floats(int rows, int head_dim) { return (rows * (head_dim + 2) + 3) / 4 * 4; }
 
-// Whether a launch shares out tiles by warps (and leaves pieces to ssd_paged_join_kernel), or whole pieces by thread blocks,
-// which loses up to a third of them where there are as many heads as a quarter of the SMs.
+// Whether a launch shares out tiles by warps, or whole pieces by thread blocks, which loses up to a third of them where there
+// are as many heads as a quarter of the SMs.
 inline bool paged_many(const PagedDecodeParams& p, int sms) { return (long long)p.c.n_seqs * p.c.H * p.qt > sms / 4; }
 
 #if defined(__CUDACC__)

@@ -7,16 +7,14 @@
 // Work: the slots of a key head are cut into tiles of 8 KB (4 KB of K, 4 KB of V).
 // Many heads (!kCta): the tiles of all (sequence, head, group) are one stream, cut into equal shares, one per warp of the
 // launch, from the lengths that the launch finds on the device.  A warp runs through the heads of its share without ever
-// meeting another; of a head that a share's border cuts it leaves a piece, (O, m, l), and a second launch joins the pieces
-// (ssd_paged_join_kernel).  Joining them here, by whoever completes the last one, was 48 us slower at 16 x 8 heads of up to
-// 32768 slots: one warp merged 15 pieces of 8 query heads while the others were done.  SMs differ by some 15% in how fast
-// their warps are served, but handing out the last eighth of the stream from a counter, in segments of three tiles and
-// more, cost more than it gave (16 x 32 E4M3 heads of up to 4224 slots 91 -> 97 us, 16 x 8 heads of up to 32768 201 -> 221):
-// every segment pays for finding its place, loading q and leaving a piece.
+// meeting another; of a head that a share's border cuts it leaves a piece, (O, m, l), in global memory.
 // Few heads (kCta): a piece is a run of tiles of one head for a whole thread block, whose warps take them in turn and merge
-// in shared memory.  The pieces of a head meet in global memory, where the thread block that completes the last one
-// (a counter, kept under the worker of the head's first piece) joins them: one launch, for the calls whose latency counts.
-// Both ways pieces are joined in the order of the workers: the result does not depend on who is first, and nobody waits.
+// in shared memory.
+// Few pieces are joined by whoever completes a head's last one (a counter, kept under the worker of its first piece: a worker
+// has one at most that starts in its share and is cut at its end), many by a second launch (ssd_paged_join_kernel,
+// p.join_later): at 16 x 8 heads of 8 query heads and up to 32768 slots, joined by the last one, one warp was merging 15
+// pieces of 8 query heads while the others were done, 48 us in all.  Both ways pieces are joined in the order of the workers:
+// the result does not depend on who is first, and nobody waits.
 //
 // A warp keeps kStages tiles of its own in shared memory and fills them with 16-byte asynchronous copies, row by row
 // (pages may have any size and strides), zeros in the place of rows that do not exist: a NaN behind the last row, or
@@ -739,7 +737,7 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
         const int skew = e * mult % (int)gridDim.x;          // head v is the business of thread block v mod gridDim
         for (int v = e * mult + ((int)blockIdx.x - skew + (skew > (int)blockIdx.x ? (int)gridDim.x : 0)); v < (e + 1) * mult; v += gridDim.x) {
           zeros(v);
-          p.pieces[v] = make_int2(0, 0);
+          if (p.join_later) p.pieces[v] = make_int2(0, 0);
         }
       }
     }
@@ -848,9 +846,34 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       if (++now.pl.t == now.pl.end) {
         w.close();
         const uint32_t w0 = worker_of(now.start), w1 = worker_of(now.start + tiles_of(now.pl.len) - 1);
-        if (lane == 0 && worker == w0) p.pieces[now.pl.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
-        if (w0 == w1) w.write_out(now.seq, now.head, now.qi);
-        else w.write_state(partial_of(worker, worker == w0), D, min(p.g - now.qi * p.rows, p.rows));
+        if (w0 == w1) {
+          if (p.join_later && lane == 0) p.pieces[now.pl.vp] = make_int2((int)w0, 1);
+          w.write_out(now.seq, now.head, now.qi);
+        } else {
+          const int n_q = min(p.g - now.qi * p.rows, p.rows);
+          w.write_state(partial_of(worker, worker == w0), D, n_q);
+          if (p.join_later) {
+            if (lane == 0 && worker == w0) p.pieces[now.pl.vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
+          } else {
+            __threadfence();
+            __syncwarp();
+            uint32_t done = 0u;
+            if (lane == 0) done = atomicAdd(p.counters + w0, 1u);
+            done = __shfl_sync(0xffffffffu, done, 0);
+            if (done == w1 - w0) {                           // the last piece: join them all
+              __threadfence();
+              if (lane == 0) p.counters[w0] = 0u;
+              for (int h = 0; h < n_q; ++h) {
+                float4 o;
+                float m, l;
+                paged_merge<D>(p, lane, h, (int)(w1 - w0 + 1), [&](int k) { return (const float*)partial_of(w0 + k, k == 0); }, o, m, l);
+                const long long qh = (long long)now.head * p.g + now.qi * p.rows + h;
+                if (lane < D / 4) paged_store4(p.out + now.seq * p.o_seq + qh * p.o_head + 8 * lane, o, paged_inverse(l), p.bf16 != 0);
+                if (lane == 0) paged_stats(p, (long long)now.seq * c.H * p.g + qh, m, l);
+              }
+            }
+          }
+        }
         if (open > 0 || more) {
           next(now);
           w.begin(now.seq, now.head, now.qi);
@@ -866,7 +889,10 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     int len = 0;
     if (tid < n_vp) {
       len = length_of(tid);
-      if (len == 0 && (uint32_t)tid % gridDim.x == blockIdx.x) zeros(tid);
+      if (len == 0 && (uint32_t)tid % gridDim.x == blockIdx.x) {
+        zeros(tid);
+        if (p.join_later) p.pieces[tid] = make_int2(0, 0);
+      }
     }
     s_len[tid] = len;
     const uint32_t tiles = tiles_of(len);
@@ -967,7 +993,9 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
           }
         }
       }
-      if (!whole) {
+      if (p.join_later) {
+        if (tid == 0 && worker == w0) p.pieces[vp] = make_int2((int)w0, (int)(w1 - w0 + 1));
+      } else if (!whole) {
         __threadfence();
         __syncthreads();
         if (tid == 0) {
