@@ -940,12 +940,15 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   // are worth a launch of their own, which spreads them over the GPU (16 query heads x 37 pieces: 62 us against 57 ..).
   const int row_b = kv->head_dim * elem_bytes(kv->dtype), tiles = (int)((p.c.cap * (long long)row_b + 4095) / 4096);
   const int heads = p.c.n_seqs * p.c.H * p.qt;
+  // About as many heads as SMs, and none long (64 tiles, eight for every warp): no shares, a thread block per head.  (8 x 16
+  // heads of 153 slots with weights: 13.0 us in two launches by shares.)
+  p.whole = heads <= sms && heads > sms / 4 && p.qt == 1 && tiles <= 64;
   const bool many = paged_many(p, sms);
   const int cuts = many ? (int)(paged_max_workers(sms) / heads) : (sms / heads < (tiles + 7) / 8 ? sms / heads : (tiles + 7) / 8);
-  p.join_later = cuts * p.rows > (many ? 16 : 128);
+  p.join_later = !p.whole && cuts * p.rows > (many ? 16 : 128);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = kv->dtype == SSD_PAGED_E4M3 ? launch_paged_decode_8(p, kv->head_dim, sms, st) : launch_paged_decode_16(p, kv->head_dim, sms, st);
-  if (e == cudaSuccess && (p.join_later || a->accumulate)) {
+  if (e == cudaSuccess && (p.join_later || (a->accumulate && !p.whole))) {
     JoinParams j = {};
     j.d = p;
     j.units = p.c.n_seqs * p.c.H * p.qt * p.rows;

@@ -167,6 +167,7 @@ struct PagedDecodeParams {
   float scale_log2;
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together
   FastDiv by_qt, by_heads;  // n / qt, n / H
+  int whole;                // 1: a head (all its query heads) per thread block, its weights added there too
   int join_later;           // 1: ssd_paged_join_kernel joins the pieces
   int whole_tiles;          // the page size is a multiple of the tile's slots
   int bf16;                 // type of q, out, k_new, v_new: 1 bf16, 0 fp16
@@ -185,7 +186,7 @@ inline int paged_part_floats(int rows, int head_dim) { return (rows * (head_dim 
 
 // Whether a launch shares out tiles by warps, or whole pieces by thread blocks, which loses up to a third of them where there
 // are as many heads as a quarter of the SMs.
-inline bool paged_many(const PagedDecodeParams& p, int sms) { return (long long)p.c.n_seqs * p.c.H * p.qt > sms / 4; }
+inline bool paged_many(const PagedDecodeParams& p, int sms) { return !p.whole && (long long)p.c.n_seqs * p.c.H * p.qt > sms / 4; }
 
 #if defined(__CUDACC__)
 constexpr float kPagedShift = 14.f;          // the weights are held 2^14 times too large, and l with them

@@ -23,8 +23,9 @@
 // Products on the tensor cores, transposed: S^T = K Q^T and O^T = V^T P^T, so that the keys and the head dimension
 // fill the 16 rows of an m16n8k16 product and the query heads its 8 columns (kNt = 2: 16 heads).  The work is bound by
 // the bytes of K and V (per 8 KB tile: 24 products and 16 ldmatrix for 8 heads, a fraction of the 8 KB's time on HBM).
-// The weights are rounded to 16 bits for the second product as a sum of two 16-bit terms, which keeps 16 (bf16) or 22
-// (fp16) bits of them; all sums are in 32 bits.  The weights are held 2^14 times too large (kPagedShift) so that the small
+// For the second product the weights are a sum of two 16-bit terms, which keeps 16 (bf16) or 22 (fp16) bits of them; over
+// 8-bit rows, whose values have 4 bits, they are one fp16 number each (11 bits; 200001 slots of 4 x 16 heads 59 -> 56 us).
+// All sums are in 32 bits.  The weights are held 2^14 times too large (kPagedShift) so that the small
 // ones of a long row stay normal numbers in fp16; the factor is in l too and cancels.
 // 8-bit rows are widened to fp16, which holds every code exactly; q is brought into fp16's range by a power of two per
 // head, the K scale multiplies the logit, and the V scale's power of two 2^e is added to it: the running maximum is that
@@ -560,7 +561,7 @@ struct Worker {
           uint32_t hi, lo;
           split2<kBf16>(w0, w1, hi, lo);
           bh[nt][hf] = transpose8(hi);
-          bl[nt][hf] = transpose8(lo);
+          if constexpr (kFmt != kPagedE4m3) bl[nt][hf] = transpose8(lo);
         }
       if constexpr (kFmt == kPagedE4m3) {
         const int vrow = sb * 16 + (mi & 1) * 8 + ml8;
@@ -575,7 +576,6 @@ struct Worker {
 #pragma unroll
             for (int nt = 0; nt < kNt; ++nt) {
               mma<kBf16>(o[nt][2 * c2 + u], a, bh[nt]);
-              mma<kBf16>(o[nt][2 * c2 + u], a, bl[nt]);
             }
           }
         }
@@ -886,42 +886,56 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
     __shared__ int s_vp, s_last;
     __shared__ float s_f[kWarps][16], s_m[16], s_l[16];
     constexpr int kPad = D + 4;                              // row of a state in shared memory: no conflicts when it is written
-    int len = 0;
-    if (tid < n_vp) {
-      len = length_of(tid);
-      if (len == 0 && (uint32_t)tid % gridDim.x == blockIdx.x) {
-        zeros(tid);
-        if (p.join_later) p.pieces[tid] = make_int2(0, 0);
+    Place pl;
+    uint32_t w0, w1, worker = blockIdx.x;                    // the workers that share this head
+    int vp, t0;
+    if (p.whole) {                                           // a head per thread block
+      vp = (int)worker;
+      pl.len = length_of(vp);
+      if (pl.len == 0) {
+        if (tid == 0) zeros(vp);
+        return;
       }
+      w0 = w1 = worker;
+      t0 = 0;
+      pl.end = (int)tiles_of(pl.len);
+    } else {
+      int len = 0;
+      if (tid < n_vp) {
+        len = length_of(tid);
+        if (len == 0 && (uint32_t)tid % gridDim.x == blockIdx.x) {
+          zeros(tid);
+          if (p.join_later) p.pieces[tid] = make_int2(0, 0);
+        }
+      }
+      s_len[tid] = len;
+      const uint32_t tiles = tiles_of(len);
+      uint32_t total, all;
+      block_scan<kThreads>(tiles, s_warp, total);
+      const uint32_t n_held = (uint32_t)__syncthreads_count(len > 0);
+      if (total == 0u) return;
+      const uint32_t workers = gridDim.x;
+      // pieces of `cut` tiles of one head each, of which there are at most `workers`: sum ceil(t / cut) <= sum t / cut + heads
+      const uint32_t cut = max((total + workers - n_held - 1) / (workers - n_held), (uint32_t)kWarps);
+      const uint32_t pieces = (tiles + cut - 1) / cut;
+      const uint32_t before = block_scan<kThreads>(pieces, s_warp, all);
+      if (worker >= all) return;
+      if (before <= worker && worker < before + pieces) s_vp = tid;
+      s_pref[tid] = before;
+      __syncthreads();
+      vp = s_vp;
+      pl.len = s_len[vp];
+      const uint32_t n_tiles = tiles_of(pl.len);
+      w0 = s_pref[vp];
+      w1 = w0 + (n_tiles - 1) / cut;
+      t0 = (int)((worker - w0) * cut);
+      pl.end = (int)min(n_tiles, t0 + cut);
     }
-    s_len[tid] = len;
-    const uint32_t tiles = tiles_of(len);
-    uint32_t total;
-    uint32_t before = block_scan<kThreads>(tiles, s_warp, total);
-    const uint32_t n_held = (uint32_t)__syncthreads_count(len > 0);
-    if (total == 0u) return;
-    const uint32_t workers = gridDim.x, worker = blockIdx.x;
-    // pieces of `cut` tiles of one head each, of which there are at most `workers`: sum ceil(t / cut) <= sum t / cut + heads
-    const uint32_t cut = max((total + workers - n_held - 1) / (workers - n_held), (uint32_t)kWarps);
-    const uint32_t pieces = (tiles + cut - 1) / cut;
-    uint32_t all;
-    before = block_scan<kThreads>(pieces, s_warp, all);
-    if (worker >= all) return;
-    if (before <= worker && worker < before + pieces) s_vp = tid;
-    s_pref[tid] = before;
-    __syncthreads();
     {
-      const int vp = s_vp;
       int seq, head, qi;
       name(vp, seq, head, qi);
       const int n_q = min(p.g - qi * p.rows, p.rows);
-      Place pl;
       pl.vp = vp;
-      pl.len = s_len[vp];
-      const uint32_t n_tiles = tiles_of(pl.len);
-      const uint32_t w0 = s_pref[vp], w1 = w0 + (n_tiles - 1) / cut;         // the workers that share this head
-      const int t0 = (int)((worker - w0) * cut);
-      pl.end = (int)min(n_tiles, t0 + cut);
       Place now = pl;
       pl.t = now.t = t0 + warp;
       const int n = pl.end > pl.t ? (pl.end - pl.t + kWarps - 1) / kWarps : 0;
@@ -991,6 +1005,18 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
             __stcg(part + p.rows * D + h, s_m[h]);
             __stcg(part + p.rows * (D + 1) + h, s_l[h]);
           }
+        }
+      }
+      if (p.whole && p.logits) {
+        // the weights, too: this thread block has all logits of the key head, and all (m, l)
+        float* scores = paged_scores(c, seq, head);
+        const float* logits = p.logits + ((long long)seq * c.H + head) * p.g * p.logit_row;
+        for (int slot = tid; slot < pl.len; slot += kThreads) {
+          float sum = 0.f;
+          for (int h = 0; h < n_q; ++h) sum += ex2(logits[h * p.logit_row + slot] - (s_m[h] - kPagedShift)) * (s_l[h] == 0.f ? 0.f : 1.f / s_l[h]);
+          if (slot >= c.score_slots) paged_flag(c, kPagedBadScores);
+          else if (p.k_new && slot == pl.len - 1) scores[slot] = sum;        // the token being appended has had none before
+          else scores[slot] += sum;
         }
       }
       if (p.join_later) {
@@ -1082,7 +1108,7 @@ cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_
     if (dev < 64) ready[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms);
+  cfg.gridDim = dim3(p.whole ? p.c.n_seqs * p.c.H * p.qt : sms);
   cfg.blockDim = dim3(G::kThreads);
   cfg.dynamicSmemBytes = G::kSmem;
   cfg.stream = st;
