@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
 // with (m, l) from the pieces.
 constexpr int kJoinWarps = kThreads / 32;
 constexpr int kAlone = 16;                          // pieces up to which one warp joins them
-constexpr int kWeightSlots = 4 * kThreads;          // slots of a thread block
+constexpr int kWeightSlots = 16 * kThreads;         // slots of a thread block
 
 __device__ __forceinline__ const float* piece_of(const PagedDecodeParams& p, int floats, int w0, int i) {
   return p.partial + ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * floats;
@@ -195,8 +195,9 @@ __device__ void join_heads(const PagedDecodeParams& p, int units, int join_block
   }
 }
 
-// The scores of kWeightSlots slots of one (sequence, key head), four neighbours per thread, eight query heads at a time:
-// their logits are on the way while each warp works out one query head's (m, l).  head_dim: that of the states in p.partial.
+// The scores of kWeightSlots slots of one (sequence, key head), four neighbours per thread and round, eight query heads at a
+// time: the first logits are on the way while each warp works out one query head's (m, l).  head_dim: that of the states in
+// p.partial.
 __device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_per_pair, int head_dim, bool joined) {
   __shared__ float2 s_ml[8];
   const PagedView& c = p.c;
@@ -204,21 +205,27 @@ __device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_pe
   const int pair = block / blocks_per_pair, part = block - pair * blocks_per_pair;
   const int seq = (int)p.by_heads.div((uint32_t)pair), head = pair - seq * c.H;
   const int len = paged_length(c, seq, head);
-  const int slot0 = part * kWeightSlots + 4 * (int)threadIdx.x;
-  if (part * kWeightSlots >= len) return;
+  const int first = part * kWeightSlots, last = min(len, first + kWeightSlots);
+  if (first >= len) return;
   float* scores = paged_scores(c, seq, head);
   const int floats = paged_part_floats(p.rows, head_dim);
-  float old[4], w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) old[i] = slot0 + i < min(len, c.score_slots) ? scores[slot0 + i] : 0.f;
   for (int h0 = 0; h0 < p.g; h0 += 8) {
-    const float* logits = p.logits + ((long long)pair * p.g + h0) * p.logit_row + slot0;
+    const float* logits = p.logits + ((long long)pair * p.g + h0) * p.logit_row;
+    const int n_h = min(8, p.g - h0);
+    const int fresh = p.k_new && h0 == 0 ? len - 1 : -1;     // the token being appended has had no weight before
     float4 x[8];
+    float old[4];
+    auto load = [&](int slot) {
 #pragma unroll
-    for (int h = 0; h < 8; ++h)
-      if (slot0 < len && h0 + h < p.g) x[h] = __ldcg(reinterpret_cast<const float4*>(logits + h * p.logit_row));
+      for (int h = 0; h < 8; ++h)
+        if (slot < last && h < n_h) x[h] = __ldcg(reinterpret_cast<const float4*>(logits + h * p.logit_row + slot));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) old[i] = slot + i < min(last, c.score_slots) && slot + i != fresh ? scores[slot + i] : 0.f;
+    };
+    int slot = first + 4 * (int)threadIdx.x;
+    load(slot);
     __syncthreads();
-    if (h0 + warp < p.g) {
+    if (warp < n_h) {
       const int qi = (h0 + warp) / p.rows, row = h0 + warp - qi * p.rows;
       const int2 pc = joined ? __ldcg(p.pieces + pair * p.qt + qi) : make_int2(0, 1);
       float2 ml;
@@ -243,23 +250,29 @@ __device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_pe
       if (lane == 0) s_ml[warp] = make_float2(ml.x, ml.y == 0.f ? 0.f : 1.f / ml.y);
     }
     __syncthreads();
+    while (slot < last) {
+      float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int h = 0; h < 8; ++h)
-      if (slot0 < len && h0 + h < p.g) {
-        const float2 ml = s_ml[h];
-        w[0] += ex2(x[h].x - ml.x) * ml.y;
-        w[1] += ex2(x[h].y - ml.x) * ml.y;
-        w[2] += ex2(x[h].z - ml.x) * ml.y;
-        w[3] += ex2(x[h].w - ml.x) * ml.y;
+      for (int h = 0; h < 8; ++h)
+        if (h < n_h) {
+          const float2 ml = s_ml[h];
+          w[0] += ex2(x[h].x - ml.x) * ml.y;
+          w[1] += ex2(x[h].y - ml.x) * ml.y;
+          w[2] += ex2(x[h].z - ml.x) * ml.y;
+          w[3] += ex2(x[h].w - ml.x) * ml.y;
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] += old[i];
+      const int at = slot;
+      slot += 4 * kThreads;
+      load(slot);                                            // the next round's, before this one's stores
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (at + i >= last) continue;
+        if (at + i >= c.score_slots) paged_flag(c, kPagedBadScores);
+        else scores[at + i] = w[i];
       }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int slot = slot0 + i;
-    if (slot >= len) continue;
-    if (slot >= c.score_slots) paged_flag(c, kPagedBadScores);
-    else if (p.k_new && slot == len - 1) scores[slot] = w[i];        // the token being appended has had none before
-    else scores[slot] = old[i] + w[i];
+    }
   }
 }
 
