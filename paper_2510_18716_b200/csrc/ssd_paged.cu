@@ -50,12 +50,19 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
   pdl_allow_successor();
   const int token = (int)(item / groups), head0 = (int)(item % groups) * kAppendHeads;
   if (token >= p.n_tokens) return;
+  // this lane's rows: head mine + it * kStep, all K or all V
+  constexpr int kStep = kRows / 2;
+  const int sub = lane / kL, part = lane % kL, mine = head0 + (sub >> 1);
+  const bool is_v = sub & 1;
   uint4 raw[kIters];                                // on the way while the token's place is looked for
+  {
+    const char* from = (is_v ? p.v_new : p.k_new) + token * p.token_b + mine * p.head_b + part * 16;
 #pragma unroll
-  for (int it = 0; it < kIters; ++it) {
-    const int r = it * kRows + lane / kL, head = head0 + (r >> 1);
-    raw[it] = make_uint4(0u, 0u, 0u, 0u);
-    if (head < c.H) raw[it] = reinterpret_cast<const uint4*>((r & 1 ? p.v_new : p.k_new) + token * p.token_b + head * p.head_b)[lane % kL];
+    for (int it = 0; it < kIters; ++it) {
+      raw[it] = make_uint4(0u, 0u, 0u, 0u);
+      if (mine + it * kStep < c.H) raw[it] = *reinterpret_cast<const uint4*>(from);
+      from += kStep * p.head_b;
+    }
   }
   int seq = token, ago = 1;
   if (p.cu) {                                       // the last sequence that begins at or before the token, 32 probes at a time
@@ -72,35 +79,45 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
     ago = p.cu[seq + 1] - token;                    // 1 for a sequence's newest token
     if (ago <= 0) return;
   }
+  // where the row goes; for all heads of the token at once where they share lengths and tables
+  const bool shared = c.n_head == 0 && c.t_head == 0;
+  char* const base = (is_v ? c.v : c.k) + part * (kQ8 ? 8 : 16);
+  char* to = base;
+  float* to_scale = is_v ? c.vs : c.ks;
+  int slot = 0;
+  bool found = false;
+  auto place = [&](int head) {
+    const int len = paged_length(c, seq, head);
+    slot = len - ago;
+    int row, page = -1;
+    if (slot >= 0) page = paged_lookup(c, paged_table(c, seq, head), slot, row);
+    else if (p.cu || len > 0) paged_flag(c, kPagedBadLength);
+    found = page >= 0;
+    if (!found) return;
+    to = base + page * c.page_b + head * c.head_b + row * c.slot_b;
+    if constexpr (kQ8) to_scale = (is_v ? c.vs : c.ks) + page * c.sc_page + head * c.sc_head + row * c.sc_slot;
+  };
+  if (shared && mine < c.H) place(mine);
 #pragma unroll
   for (int it = 0; it < kIters; ++it) {
-    const int r = it * kRows + lane / kL, head = head0 + (r >> 1), part = lane % kL;
-    bool ok = head < c.H;
-    int page = 0, row = 0;
-    if (ok) {
-      const int len = paged_length(c, seq, head);
-      const int slot = len - ago;
-      ok = slot >= 0;
-      if (!ok && (p.cu || len > 0)) paged_flag(c, kPagedBadLength);
-      if (ok) {
-        page = paged_lookup(c, paged_table(c, seq, head), slot, row);
-        ok = page >= 0;
-        if (ok && c.scores && part == 0 && !(r & 1)) {
-          if (slot < c.score_slots) paged_scores(c, seq, head)[slot] = 0.f;
-          else paged_flag(c, kPagedBadScores);
-        }
-      }
-    }
-    char* to = (r & 1 ? c.v : c.k) + page * c.page_b + head * c.head_b + row * c.slot_b;
+    const int head = mine + it * kStep;
+    if (!shared && head < c.H) place(head);
+    const bool ok = found && head < c.H;
     if constexpr (kQ8) {
       float scale;
       const uint2 code = paged_quantize<kL>(raw[it], p.bf16 != 0, scale);
       if (ok) {
-        reinterpret_cast<uint2*>(to)[part] = code;
-        if (part == 0) (r & 1 ? c.vs : c.ks)[page * c.sc_page + head * c.sc_head + row * c.sc_slot] = scale;
+        *reinterpret_cast<uint2*>(to) = code;
+        if (part == 0) *to_scale = scale;
       }
+      to_scale += kStep * c.sc_head;
     } else if (ok) {
-      reinterpret_cast<uint4*>(to)[part] = raw[it];
+      *reinterpret_cast<uint4*>(to) = raw[it];
+    }
+    to += kStep * c.head_b;
+    if (ok && c.scores && part == 0 && !is_v) {     // a new token has had no weight yet
+      if (slot < c.score_slots) paged_scores(c, seq, head)[slot] = 0.f;
+      else paged_flag(c, kPagedBadScores);
     }
   }
 }

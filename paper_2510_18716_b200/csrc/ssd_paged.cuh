@@ -104,16 +104,20 @@ __device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, flo
   float x[8], m = 0.f;
   widen8(raw, bf16, x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));     // a NaN is passed over
+  // not negative, so the bit patterns order like the values
+  uint32_t top = __float_as_uint(m);
 #pragma unroll
-  for (int o = kLanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  scale = __fdiv_rn(m, 448.f);
+  for (int o = kLanes / 2; o >= 1; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  m = __uint_as_float(top);
+  // Quotients, correctly rounded, from the correctly rounded reciprocal of the divisor and one remainder (Markstein, IBM J.
+  // Res. Dev. 34, 1990): three operations per value instead of a division.  The theorem leaves out divisors whose significand
+  // is all ones, and wants nothing to overflow or underflow; where it does not hold, divide.
+  const bool sane = m > 0x1p-80f && m < 0x1p80f;
+  constexpr float r448 = 1.f / 448.f;
+  const float y448 = m * r448;
+  scale = sane ? fmaf(fmaf(-y448, 448.f, m), r448, y448) : __fdiv_rn(m, 448.f);
   const float by = scale > 0.f ? scale : 1.f;
-  // x / by, correctly rounded, from the correctly rounded reciprocal and one remainder (Markstein, IBM J. Res. Dev. 34,
-  // 1990): three operations per value instead of a division.  The theorem leaves out divisors whose significand is all
-  // ones, and wants nothing to overflow or underflow; where it does not hold, divide.
-  const uint32_t bits = __float_as_uint(by);
-  const bool plain = by > 0x1p-100f && by < 0x1p100f && (bits & 0x7fffffu) != 0x7fffffu;
   const float r = __frcp_rn(by);
   float q[8];
 #pragma unroll
@@ -121,7 +125,7 @@ __device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, flo
     const float y = x[i] * r;
     q[i] = fmaf(fmaf(-y, by, x[i]), r, y);
   }
-  if (!plain) {
+  if (!sane || (__float_as_uint(by) & 0x7fffffu) == 0x7fffffu) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(x[i], by);
   }
