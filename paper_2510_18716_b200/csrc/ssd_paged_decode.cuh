@@ -417,7 +417,8 @@ struct Worker {
     constexpr int kSub = G::kTile / 16;
     const uint32_t base = ring + stage * G::kStage;
     const unsigned char* mem = ring_ptr + stage * G::kStage;
-    float s[kSub][kNt][4], s2[kSub][kNt][4];                 // two sums, so that a product need not wait for the one before
+    constexpr bool kTwo = kSub * kNt == 1;                   // one chain of products: two sums, so that one need not wait for the other
+    float s[kSub][kNt][4], s2[kSub][kNt][4];
     float vinv[kSub][2], vman[kSub][2];                      // 2^-e, and the V scale times that
     const int j8 = lane >> 2, mi = lane >> 3, ml8 = lane & 7;
 #pragma unroll
@@ -436,7 +437,7 @@ struct Worker {
           for (int u = 0; u < 2; ++u) {
             const uint32_t a[4] = {widen_lo(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u]), widen_hi(r[2 * u + 1])};
 #pragma unroll
-            for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(u == 0 ? s[sb][nt] : s2[sb][nt], a, qf[nt][2 * c2 + u]);
+            for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(u == 0 || !kTwo ? s[sb][nt] : s2[sb][nt], a, qf[nt][2 * c2 + u]);
           }
         }
       } else {
@@ -445,7 +446,7 @@ struct Worker {
           uint32_t a[4];
           ldsm4(a, base + chunk_at(krow, 2 * ks + (mi >> 1)));
 #pragma unroll
-          for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(ks % 2 == 0 ? s[sb][nt] : s2[sb][nt], a, qf[nt][ks]);
+          for (int nt = 0; nt < kNt; ++nt) mma<kBf16>(ks % 2 == 0 || !kTwo ? s[sb][nt] : s2[sb][nt], a, qf[nt][ks]);
         }
       }
     }
@@ -463,7 +464,7 @@ struct Worker {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float& x = s[sb][nt][2 * hf + e];
-            x += s2[sb][nt][2 * hf + e];
+            if (kTwo) x += s2[sb][nt][2 * hf + e];
             x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kPagedNegInf;
           }
       }
