@@ -498,7 +498,7 @@ class PagedKV:
             raise ValueError(f"PagedKV: the table has rows for {heads} heads, the pages for {pool_heads}")
         if lengths.dtype != torch.int32 or tuple(lengths.shape) not in ((n_seqs,), (n_seqs, heads)):
             raise ValueError(f"PagedKV: want lengths int32 [{n_seqs}] or [{n_seqs}, {heads}]")
-        if min(k_pages.shape) < 1 or page_table.shape[-1] < 1:
+        if min(k_pages.shape) < 1 or min(page_table.shape) < 1:
             raise ValueError("PagedKV: empty pages or an empty table")
         if _strides(k_pages, 3) != _strides(v_pages, 3) or k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
             raise ValueError("PagedKV: k_pages and v_pages need the same strides, the last dimension contiguous")

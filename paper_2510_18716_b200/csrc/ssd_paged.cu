@@ -933,8 +933,9 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   p.qt = (p.g + p.rows - 1) / p.rows;
   p.by_qt = fast_div((uint32_t)p.qt);
   p.by_heads = fast_div((uint32_t)kv->n_kv_heads);
-  // tiles are counted in 32 bits (a tile has 16 slots at least)
-  if ((double)kv->n_seqs * kv->n_kv_heads * p.qt * (p.c.cap / 16 + 1) > 2.0e9) return SSD_ERR_LIMIT;
+  // tiles (of 16 slots at least, and two more per head) and query heads are counted in 31 bits
+  const double n_heads = (double)kv->n_seqs * kv->n_kv_heads * p.qt;
+  if (n_heads * (p.c.cap / 16 + 4) > 2.0e9 || n_heads * p.rows > 1.0e9) return SSD_ERR_LIMIT;
   if (kv->n_seqs == 0) return SSD_OK;
   int sms = 0;
   rc = sm_count(&sms);
@@ -1011,7 +1012,8 @@ extern "C" int ssd_paged_append(const ssd_paged_kv* kv, const void* k_new, const
   AppendPagedParams p = {};
   const int rc = check_view(kv, &p.c);
   if (rc != SSD_OK) return rc;
-  if (!k_new || !v_new || n_tokens < 0 || (!cu_seqlens && n_tokens != kv->n_seqs)) return SSD_ERR_INVALID_ARG;
+  if (n_tokens < 0 || (!cu_seqlens && n_tokens != kv->n_seqs)) return SSD_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!k_new || !v_new)) return SSD_ERR_INVALID_ARG;
   if (new_dtype != SSD_PAGED_BF16 && new_dtype != SSD_PAGED_FP16) return SSD_ERR_INVALID_ARG;
   if (kv->dtype != SSD_PAGED_E4M3 && new_dtype != kv->dtype) return SSD_ERR_INVALID_ARG;
   if (new_token_stride < 0 || new_head_stride < 0 || new_token_stride > (int64_t)1 << 48 || new_head_stride > (int64_t)1 << 48 ||

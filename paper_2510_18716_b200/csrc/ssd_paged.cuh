@@ -123,7 +123,7 @@ __device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, flo
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float y = x[i] * r;
-    q[i] = fmaf(fmaf(-y, by, x[i]), r, y);
+    q[i] = copysignf(fmaf(fmaf(-y, by, x[i]), r, y), x[i]);  // the sign of a zero is lost on the way
   }
   if (!sane || (__float_as_uint(by) & 0x7fffffu) == 0x7fffffu) {
 #pragma unroll

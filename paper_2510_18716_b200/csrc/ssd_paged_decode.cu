@@ -3,9 +3,7 @@
 
 namespace ssd {
 
-size_t paged_max_workers(int sms) {
-  return (size_t)sms * (SSD_PAGED_WARPS8 > SSD_PAGED_WARPS16 ? SSD_PAGED_WARPS8 : SSD_PAGED_WARPS16);
-}
+size_t paged_max_workers(int sms) { return (size_t)sms * (paged::kWarps8 > paged::kWarps16 ? paged::kWarps8 : paged::kWarps16); }
 
 cudaError_t launch_paged_decode_16(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st) {
   if (p.bf16)

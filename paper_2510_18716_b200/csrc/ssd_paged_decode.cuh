@@ -40,16 +40,16 @@ namespace ssd {
 namespace paged {
 
 
-#ifndef SSD_PAGED_WARPS16
-#define SSD_PAGED_WARPS16 8
-#define SSD_PAGED_WARPS8 12
-#define SSD_PAGED_STAGES 2
-#endif
+// Warps of a thread block (one to an SM) and stages of a warp.  8 x 2 x 8 KB in flight feed 16-bit rows; more make them
+// slower (16 x 8 heads of up to 32768 slots: 8 warps 183 us, 10 192, 12 200; three stages 208), fewer do not keep up.
+// 8-bit rows have twice the values per byte to widen and take 12 warps (16 x 32 heads of up to 4224 slots: 8 warps 117 us,
+// 10 93, 12 87), except for 16 query heads, whose state needs the registers of 8.
+constexpr int kWarps16 = 8, kWarps8 = 12;
 template <int D, int kFmt, int kNt>
 struct Geo {
-  static constexpr int kWarps = kFmt == kPagedE4m3 && kNt == 1 ? SSD_PAGED_WARPS8 : SSD_PAGED_WARPS16;
+  static constexpr int kWarps = kFmt == kPagedE4m3 && kNt == 1 ? kWarps8 : kWarps16;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kStages = SSD_PAGED_STAGES;
+  static constexpr int kStages = 2;
   static constexpr int kRow = kFmt == kPagedE4m3 ? D : 2 * D;      // bytes of a row in a page
   static constexpr int kTile = 4096 / kRow;                        // keys of a tile
   static constexpr int kCpr = kRow / 16;                           // 16-byte chunks of a row
@@ -409,7 +409,10 @@ struct Worker {
       if (store) reinterpret_cast<uint4*>(to)[part] = raw;
     }
     // the new token has had no weight yet (where this step's weights are wanted, their kernel starts it)
-    if (store && c.scores && !p.logits && lane == 0 && at.len <= c.score_slots) paged_scores(c, seq, head)[at.len - 1] = 0.f;
+    if (store && c.scores && !p.logits && lane == 0) {
+      if (at.len <= c.score_slots) paged_scores(c, seq, head)[at.len - 1] = 0.f;
+      else paged_flag(c, kPagedBadScores);
+    }
   }
 
   // ---------------------------------------------------------------- one tile

@@ -8,8 +8,10 @@ rounding of a weight 2^-17 (bf16: 2^-9 twice, and a margin of two; fp16 less; ov
 whose rounding is off by 2^-11 at most), the sums over n slots at most n u relative to
 the sum of the absolute terms, merging and the final division 2^-21.  So a weight is off by at most
     delta = D 2^-23 A + 8 u A + 2^-17 (8 bits: 2^-11) + n u + 2^-20     (relative)
-and twice that after the division by the sum, which has the same error.  An output is off by 2 delta sum w |v| and its own
-rounding, half a step: eps/2 |o|.  An accumulated score is off by 2 delta of the weights added and u of its value for each
+and twice that after the division by the sum, which has the same error.  In fp16 (fp16 and 8-bit pages) a weight also has an
+absolute error: the largest is held at 2^14, the smallest step is 2^-24, so half a step is 2^-39 of the largest; with a margin
+of two an output is off by 2^-38 max(w) sum |v| on that account (8 bits: 2^-38 max(w scale) sum |code|, the scale being part
+of the weight there).  An output is off by 2 delta sum w |v|, that, and its own rounding, half a step: eps/2 |o|.  An accumulated score is off by 2 delta of the weights added and u of its value for each
 of the g + 1 additions; a log of the sum by delta and 4 u of its value.
 """
 import math
@@ -89,6 +91,12 @@ class Paged:
         x = x.double()
         return x if self.dtype != "e4m3" else x * self.scales[which][pg, hh, r].double()[:, None]
 
+    def row_scales(self, i, h):
+        """V's scales of a head."""
+        s = np.arange(int(self.n[i, h]))
+        pg = torch.from_numpy(self.table_np[i, h % self.table_np.shape[1]][s // self.page].astype(np.int64)).cuda()
+        return self.scales[1][pg, h % self.pages[1].shape[1], torch.from_numpy(s % self.page).cuda()].double().clamp(min=1e-300)
+
     def bits(self):
         got = [p.contiguous().view(torch.uint8).clone() for p in self.pages]
         return got + [s.contiguous().view(torch.uint8).clone() for s in self.scales if s is not None]
@@ -120,7 +128,13 @@ def reference(c, q, scale=None):
             delta = c.d * 2.0 ** -23 * a + 8 * U * a + (2.0 ** -11 if c.dtype == "e4m3" else 2.0 ** -17) + n * U + 2.0 ** -20
             o = w @ v
             out[i, h * g:(h + 1) * g] = o
-            e_out[i, h * g:(h + 1) * g] = half * o.abs() + 2 * delta * (w @ v.abs()) + torch.finfo(q.dtype).tiny
+            floor = 0.0
+            if c.dtype == "fp16":
+                floor = 2.0 ** -38 * w.amax(dim=1, keepdim=True) * v.abs().sum(dim=0)
+            elif c.dtype == "e4m3":
+                s = c.row_scales(i, h)
+                floor = 2.0 ** -38 * (w * s).amax(dim=1, keepdim=True) * (v / s[:, None]).abs().sum(dim=0)
+            e_out[i, h * g:(h + 1) * g] = half * o.abs() + 2 * delta * (w @ v.abs()) + floor + torch.finfo(q.dtype).tiny
             lse[i, h * g:(h + 1) * g] = (m + z.log())[:, 0]
             e_lse[i, h * g:(h + 1) * g] = (delta + 4 * U * ((m + z.log()).abs() + 16))[:, 0]
             w_all[i, h, :n] = w.sum(dim=0)
@@ -221,6 +235,40 @@ def test_one_long_sequence_among_short_ones():
     check_attention(c, q, out, lse, before=before)
 
 
+@pytest.mark.parametrize("n_seqs,heads,per_head", [(3000, 4, False), (700, 5, True)])
+def test_more_sequences_than_threads(n_seqs, heads, per_head):
+    r = np.random.RandomState(n_seqs)
+    n = r.randint(0, 40, size=(n_seqs, heads) if per_head else n_seqs) * r.randint(0, 2, size=(n_seqs, 1) if per_head else n_seqs)
+    c = Paged(n, heads, d=64, per_head=per_head, scores=True, page=8)
+    q, before = new_q(c, 2), c.scores.clone()
+    out, lse = c.kv.decode_attn(q, return_lse=True, accumulate=True)
+    # plain arithmetic for all of them at once, on the cache's rows padded to the longest
+    top = int(c.n.max())
+    slot = torch.arange(top, device="cuda").expand(n_seqs, heads, -1)
+    table = torch.from_numpy(np.broadcast_to(c.table_np, (n_seqs, heads, c.table_np.shape[2])).astype(np.int64)).cuda()
+    held = slot < torch.from_numpy(c.n).cuda()[..., None]
+    at = (torch.gather(table, 2, slot // 8).clamp(min=0), torch.arange(c.pages[0].shape[1], device="cuda").view(1, -1, 1).expand_as(slot), slot % 8)
+    k, v = (torch.where(held[..., None], p[at].double(), torch.zeros((), dtype=torch.float64, device="cuda")) for p in c.pages)
+    x = q.double().view(n_seqs, heads, 2, 64) @ k.transpose(2, 3) / 8.0
+    x = torch.where(held[:, :, None], x, torch.full_like(x, -math.inf))
+    w = torch.nan_to_num(torch.softmax(x, dim=3), nan=0.0)
+    want = (w @ v).view(n_seqs, 2 * heads, 64)
+    # A <= |q| |k| scale <= 50 here: delta <= 64 2^-23 50 + .. < 5e-4
+    bound = 2.0 ** -8 * want.abs() + 1e-3 * (w @ v.abs()).view(n_seqs, 2 * heads, 64) + 1e-30
+    assert bool(((out.double() - want).abs() <= bound).all())
+    err = (c.scores[..., :top].double() - before[..., :top].double() - w.sum(dim=2)).abs()
+    assert bool((err <= 1e-3 * w.sum(dim=2) + 4 * U * before[..., :top].abs() + 1e-12).all())
+    assert c.kv.device_status() == 0
+
+
+@pytest.mark.parametrize("g,n_seqs", [(128, 3), (40, 30)])
+def test_very_large_groups(g, n_seqs):
+    c = Paged([200, 17, 90] * (n_seqs // 3), 1, scores=True)
+    q, before = new_q(c, g), c.scores.clone()
+    out, lse = c.kv.decode_attn(q, return_lse=True, accumulate=True)
+    check_attention(c, q, out, lse, before=before)
+
+
 def test_all_sequences_empty():
     c = Paged([0, 0, 0], 4, scores=True)
     q, before = new_q(c, 2), c.scores.clone()
@@ -236,7 +284,8 @@ def test_large_logits_and_scales(dtype):
     """Logits of some hundred and rows of very different size: weights from one slot only down to nothing."""
     c = Paged([400, 33, 1000], 2, dtype=dtype, seed=5)
     if dtype == "e4m3":
-        c.scales[1].mul_(torch.exp2(torch.randint(-40, 20, c.scales[1].shape, device="cuda").float()))
+        g = torch.Generator(device="cuda").manual_seed(29)
+        c.scales[1].mul_(torch.exp2(torch.randint(-40, 20, c.scales[1].shape, generator=g, device="cuda").float()))
     q = new_q(c, 4) * 64
     out, lse = c.kv.decode_attn(q, return_lse=True)
     check_attention(c, q, out, lse)
@@ -402,6 +451,57 @@ def test_append(dtype, d, heads, order, per_head):
     want = expect_append(c, k, v, np.arange(7))
     c.kv.append(k, v)
     assert_cache(c, want)
+    assert c.kv.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_codes_of_rows_of_any_size(dtype, d):
+    """Scales and codes are correctly rounded quotients over the whole range of the types, zero, denormal and border values
+    included."""
+    n_rows = 20000
+    g = torch.Generator(device="cuda").manual_seed(d)
+    t = TYPES[dtype]
+    span = 60 if dtype == "bf16" else 12
+    x = torch.randn((n_rows, 1, d), generator=g, device="cuda") * torch.exp2(torch.randint(-2 * span, span, (n_rows, 1, 1), generator=g, device="cuda").float())
+    x[::3] *= torch.exp2(torch.randint(-12, 1, x[::3].shape, generator=g, device="cuda").float())
+    x[::7] = torch.round(x[::7] * 16) / 16                           # halves between codes, exactly
+    x[5], x[6] = 0.0, torch.finfo(t).max
+    x[7], x[8, 0, 3:] = torch.finfo(t).smallest_normal / 4, 0.0
+    x = x.clamp(-torch.finfo(t).max, torch.finfo(t).max).to(t)
+    c = Paged([n_rows], 1, d=d, dtype="e4m3", page=64)
+    c.kv.append(x, x, torch.tensor([0, n_rows], dtype=torch.int32, device="cuda"))
+    code, scale = quantized(x)
+    got = [torch.from_numpy(np.arange(n_rows)).cuda()]
+    at = (torch.from_numpy(c.table_np[0, 0].astype(np.int64)).cuda()[got[0] // 64], 0, got[0] % 64)
+    for w in range(2):
+        assert torch.equal(c.scales[w][at], scale[:, 0])
+        bad = (c.pages[w].view(torch.uint8)[at] != code[:, 0].view(torch.uint8)).nonzero()
+        assert len(bad) == 0, [(r, i, float(x[r, 0, i]), float(scale[r, 0])) for r, i in bad[:5].tolist()]
+    if dtype == "bf16" and d == 128:                                 # and the slab cache's quantiser says the same
+        codes, scales = B.quantize_rows_e4m3(x[:, 0].contiguous())
+        assert torch.equal(codes, code[:, 0].view(torch.uint8)) and torch.equal(scales, scale[:, 0])
+
+
+def test_append_for_many_sequences():
+    r = np.random.RandomState(1)
+    tokens = r.randint(0, 4, size=2500) * r.randint(0, 2, size=2500)
+    n = tokens + r.randint(0, 5, size=2500)
+    c = Paged(n, 2, d=64, page=8, scores=True)
+    cu = np.concatenate([[0], np.cumsum(tokens)])
+    new = torch.randn((int(cu[-1]), 2, 64), generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").to(torch.bfloat16)
+    seq = np.repeat(np.arange(2500), tokens)
+    slot = n[seq] - tokens[seq] + (np.arange(len(seq)) - cu[seq])
+    page = torch.from_numpy(c.table_np[seq, 0, slot // 8].astype(np.int64)).cuda()
+    at = torch.from_numpy(slot % 8).cuda()
+    pages, scores = [p.clone() for p in c.pages], c.scores.clone()
+    for p in pages:
+        p[page, :, at] = new
+    scores[torch.from_numpy(seq).cuda(), :, torch.from_numpy(slot).cuda()] = 0
+    c.kv.append(new, new, torch.from_numpy(cu.astype(np.int32)).cuda())
+    assert_cache(c, (pages, c.scales, scores))
+    c.kv.append(new[:0], new[:0], torch.zeros(2501, dtype=torch.int32, device="cuda"))       # no new tokens at all
+    assert_cache(c, (pages, c.scales, scores))
     assert c.kv.device_status() == 0
 
 
@@ -607,6 +707,34 @@ def test_captured_step_follows_lengths_and_pages():
     c.n += 5
     want, _, _, e_out, _, _ = reference(c, q)
     assert bool(((out.double() - want).abs() <= e_out).all())
+
+
+@pytest.mark.parametrize("cap", [64, 2048])
+def test_captured_refresh(cap):
+    """Append, attention with weights and eviction in one captured graph, replayed: the same bits as the calls one by one."""
+    made = [Paged([50, 20, 0, 61], 4, dtype="e4m3", scores=True, room=cap - 61) for _ in range(2)]
+    q, new = new_q(made[0], 2), torch.randn((4, 4, 128), device="cuda").to(torch.bfloat16)
+    for c in made:
+        c.kv.reserve(8, accumulate=True)
+        c.heads_len = torch.from_numpy(np.repeat(c.n[:, :1], 4, 1).astype(np.int32)).cuda()
+        c.kv = B.PagedKV(c.pages[0], c.pages[1], c.table, c.heads_len, k_scales=c.scales[0], v_scales=c.scales[1], scores=c.scores)
+        c.kv.reserve(8, accumulate=True)
+    a, b = made
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        a.heads_len.add_((a.heads_len > 0).int())
+        out = a.kv.append_decode(new, new, q, accumulate=True)
+        kept = a.kv.evict(4, [20, 30, 0, 5], [10, 8, 40, 30])
+    for step in range(4):
+        q.copy_(new_q(b, 2, seed=step + 50))
+        new.copy_(torch.randn(new.shape, device="cuda"))
+        g.replay()
+        b.heads_len.add_((b.heads_len > 0).int())
+        want = b.kv.append_decode(new, new, q, accumulate=True)
+        want_kept = b.kv.evict(4, [20, 30, 0, 5], [10, 8, 40, 30])
+        assert torch.equal(out, want) and torch.equal(kept, want_kept) and torch.equal(a.heads_len, b.heads_len)
+        assert_cache(a, (b.pages, b.scales, b.scores))
+    assert b.kv.device_status() == 0 and b.heads_len.max().item() <= 44
 
 
 def test_capture_needs_a_reserved_workspace():

@@ -79,6 +79,13 @@ def test_bad_attention_arguments(change):
     assert lib.ssd_paged_append_decode(kv(), attn(**change), None) == B.SSD_ERR_INVALID_ARG
 
 
+def test_more_query_heads_than_can_be_counted():
+    lib = B.load()
+    many = 8 << 26
+    assert lib.ssd_paged_decode_attn(kv(), attn(n_q_heads=many), None) == B.SSD_ERR_LIMIT
+    assert lib.ssd_paged_append_decode(kv(max_pages=1 << 20), attn(n_q_heads=8 << 16), None) == B.SSD_ERR_LIMIT
+
+
 def test_bad_arguments_of_single_calls():
     lib = B.load()
     bad = B.SSD_ERR_INVALID_ARG
@@ -89,6 +96,7 @@ def test_bad_arguments_of_single_calls():
     append = lambda view=kv(), k=AT, v=AT, t=0, ts=1024, hs=128, cu=None, n=2: lib.ssd_paged_append(view, k, v, t, ts, hs, cu, n, None)  # noqa: E731
     assert append(k=None) == append(v=None) == append(k=AT + 2) == append(t=1) == append(t=2) == append(ts=-8) == append(hs=4) == bad
     assert append(n=3) == append(n=-1) == append(cu=AT + 2, n=3) == append(view=None) == bad
+    assert append(cu=AT, n=0, k=None, v=None) == B.SSD_OK            # a step without new tokens
     ints = lambda x: (C.c_int32 * 8)(*([x] * 8))  # noqa: E731
 
     def evict(view=None, into=None, prefix=4, b=ints(8), r=ints(4), kept=AT, cols=16, counts=AT):
@@ -129,3 +137,5 @@ def test_the_handle_refuses_what_is_not_on_a_gpu():
         B.PagedKV(k, k, t, n, scores=torch.zeros(1, 3, 8))
     with pytest.raises(ValueError, match="heads"):
         B.PagedKV(k, k, torch.zeros(1, 4, 2, dtype=torch.int32), n)
+    with pytest.raises(ValueError, match="empty"):
+        B.PagedKV(k, k, torch.zeros(0, 2, dtype=torch.int32), torch.zeros(0, dtype=torch.int32))
