@@ -172,6 +172,7 @@ struct PagedDecodeParams {
   int g, qt, rows;          // query heads per key head; groups of at most `rows` of them that one worker takes together
   FastDiv by_qt, by_heads;  // n / qt, n / H
   int whole;                // 1: a head (all its query heads) per thread block, its weights added there too
+  int split;                // few heads, short: thread blocks per head; 0: shares by the lengths
   int join_later;           // 1: ssd_paged_join_kernel joins the pieces
   int whole_tiles;          // the page size is a multiple of the tile's slots
   int bf16;                 // type of q, out, k_new, v_new: 1 bf16, 0 fp16

@@ -910,6 +910,19 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
       w0 = w1 = worker;
       t0 = 0;
       pl.end = (int)tiles_of(pl.len);
+    } else if (p.split > 0) {                                // `split` thread blocks per head, a tile for each of their warps
+      vp = (int)worker / p.split;
+      pl.len = length_of(vp);
+      const int part = (int)worker - vp * p.split, n_tiles = (int)tiles_of(pl.len);
+      if (pl.len == 0 && part == 0 && tid == 0) {
+        zeros(vp);
+        if (p.join_later) p.pieces[vp] = make_int2(0, 0);
+      }
+      t0 = part * kWarps;
+      if (t0 >= n_tiles) return;
+      pl.end = min(n_tiles, t0 + kWarps);
+      w0 = (uint32_t)(vp * p.split);
+      w1 = w0 + (uint32_t)((n_tiles - 1) / kWarps);
     } else {
       int len = 0;
       if (tid < n_vp) {
@@ -1105,8 +1118,18 @@ __global__ void __launch_bounds__(Geo<D, kFmt, kNt>::kThreads, 1) ssd_paged_deco
 }
 
 template <int D, int kFmt, int kNt, bool kCta>
-cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_t st) {
+cudaError_t launch_paged_kernel(const PagedDecodeParams& in, int sms, cudaStream_t st) {
   using G = Geo<D, kFmt, kNt>;
+  PagedDecodeParams p = in;
+  int grid = sms;
+  if (kCta) {
+    // Where one tile per warp is not more than the SMs can take, thread blocks are assigned without looking at the lengths,
+    // and the SMs that are left over can start the next launch (8 heads of 613 slots: 8.6 us with a grid of all SMs).
+    const int heads = p.c.n_seqs * p.c.H * p.qt;
+    const int tiles = (p.c.cap + G::kTile - 1) / G::kTile, split = (tiles + G::kWarps - 1) / G::kWarps;
+    if (p.whole) grid = heads;
+    else if ((long long)heads * split <= sms) grid = heads * (p.split = split);
+  }
   auto* kernel = ssd_paged_decode_kernel<D, kFmt, kNt, kCta>;
   // once per device; host threads that meet here make the same idempotent call
   static std::atomic<bool> ready[64] = {};
@@ -1119,7 +1142,7 @@ cudaError_t launch_paged_kernel(const PagedDecodeParams& p, int sms, cudaStream_
     if (dev < 64) ready[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.whole ? p.c.n_seqs * p.c.H * p.qt : sms);
+  cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(G::kThreads);
   cfg.dynamicSmemBytes = G::kSmem;
   cfg.stream = st;
