@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
 // with (m, l) from the pieces.
 constexpr int kJoinWarps = kThreads / 32;
 constexpr int kAlone = 16;                          // pieces up to which one warp joins them
-constexpr int kWeightSlots = 16 * kThreads;         // slots of a thread block
+constexpr int kWeightSlots = 4 * kThreads;          // slots of a thread block's round: it makes one, two or four
 
 __device__ __forceinline__ const float* piece_of(const PagedDecodeParams& p, int floats, int w0, int i) {
   return p.partial + ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * floats;
@@ -212,17 +212,17 @@ __device__ void join_heads(const PagedDecodeParams& p, int units, int join_block
   }
 }
 
-// The scores of kWeightSlots slots of one (sequence, key head), four neighbours per thread and round, eight query heads at a
+// The scores of `slots` slots of one (sequence, key head), four neighbours per thread and round, eight query heads at a
 // time: the first logits are on the way while each warp works out one query head's (m, l).  head_dim: that of the states in
 // p.partial.
-__device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_per_pair, int head_dim, bool joined) {
+__device__ void add_weights(const PagedDecodeParams& p, int block, int blocks_per_pair, int slots, int head_dim, bool joined) {
   __shared__ float2 s_ml[8];
   const PagedView& c = p.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int pair = block / blocks_per_pair, part = block - pair * blocks_per_pair;
   const int seq = (int)p.by_heads.div((uint32_t)pair), head = pair - seq * c.H;
   const int len = paged_length(c, seq, head);
-  const int first = part * kWeightSlots, last = min(len, first + kWeightSlots);
+  const int first = part * slots, last = min(len, first + slots);
   if (first >= len) return;
   float* scores = paged_scores(c, seq, head);
   const int floats = paged_part_floats(p.rows, head_dim);
@@ -297,6 +297,7 @@ struct JoinParams {
   PagedDecodeParams d;
   int join_blocks, units, blocks_per_pair;   // the thread blocks after the first join_blocks add weights
   int one_each;                              // a query head per thread block, instead of one per warp
+  int slots;                                 // of a thread block that adds weights
 };
 
 template <int D>
@@ -304,7 +305,7 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_join_kernel(const __grid_c
   pdl_wait_predecessor();
   pdl_allow_successor();
   if ((int)blockIdx.x < p.join_blocks) join_heads<D>(p.d, p.units, p.join_blocks, p.one_each != 0);
-  else add_weights(p.d, blockIdx.x - p.join_blocks, p.blocks_per_pair, D, p.join_blocks > 0);
+  else add_weights(p.d, blockIdx.x - p.join_blocks, p.blocks_per_pair, p.slots, D, p.join_blocks > 0);
 }
 
 // ----------------------------------------------------------------------------- eviction: which tokens stay
@@ -985,7 +986,11 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
     j.units = p.c.n_seqs * p.c.H * p.qt * p.rows;
     j.one_each = j.units <= 4 * sms;
     j.join_blocks = p.join_later ? (j.one_each ? j.units : (j.units + kJoinWarps - 1) / kJoinWarps) : 0;
-    j.blocks_per_pair = (p.c.cap + kWeightSlots - 1) / kWeightSlots;
+    // rounds that follow one another hide their loads, but not where they leave SMs without work
+    const long long pairs = (long long)p.c.n_seqs * p.c.H;
+    j.slots = kWeightSlots;
+    while (j.slots < 4 * kWeightSlots && pairs * ((p.c.cap + j.slots - 1) / j.slots) > 4 * sms) j.slots *= 2;
+    j.blocks_per_pair = (p.c.cap + j.slots - 1) / j.slots;
     const int blocks = j.join_blocks + (a->accumulate ? p.c.n_seqs * p.c.H * j.blocks_per_pair : 0);
     e = launch<JoinParams>(kv->head_dim == 128 ? ssd_paged_join_kernel<128> : ssd_paged_join_kernel<64>, dim3((unsigned)blocks), kThreads, 0, st, j);
   }
