@@ -475,11 +475,11 @@ __device__ __forceinline__ void emit(uint32_t t, uint32_t budget, int prefix, in
 }
 
 // The choice of a (sequence, head) among at most kT * kK candidates, in registers: the smallest key to be taken bit by bit.
+// s_key: kT * kK values of shared memory.
 template <int kT, int kK>
-__device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHead& e, int32_t* out) {
+__device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHead& e, uint32_t* s_key, int32_t* out) {
   constexpr int kW = kT / 32;
   __shared__ uint32_t s_count[2][kW];
-  __shared__ uint32_t s_key[kT * kK];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
   const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;       // of a warp
@@ -730,7 +730,8 @@ template <int kRow, bool kInPlace, int kT>
 __global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_constant__ EvictParams p) {
   constexpr int kWarps = kT / 32, kCpr = kRow / 16, kL = 2 * kCpr, kRpi = 32 / kL, kU = 8;
   __shared__ int32_t s_kept[kShort];
-  __shared__ long long s_src[kShort], s_dst[kShort];         // bytes from the head's first row; source -1: nothing to move
+  __shared__ int32_t s_from[kShort], s_to[kShort];           // pages; -1: nothing to move.  (s_from: the keys, before that)
+  __shared__ uint32_t s_rows[kShort];                        // rows in them, the source's in the low half (below kShort both)
   const PagedView& a = p.src;
   const PagedView& b = p.dst;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -742,7 +743,7 @@ __global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_
   for (int j = tid; j < (e.all ? e.n : p.prefix); j += kT) s_kept[j] = j;
   if (!e.all)
     for (int j = tid; j < e.recent; j += kT) s_kept[p.prefix + e.budget + j] = e.n - e.recent + j;
-  if (chosen) choose_short<kT, kShort / kT>(p, e, s_kept + p.prefix);
+  if (chosen) choose_short<kT, kShort / kT>(p, e, reinterpret_cast<uint32_t*>(s_from), s_kept + p.prefix);
   __syncthreads();                                           // the list is complete, and every warp has read the length
   if (tid == 0) {
     p.counts[pair] = e.count;
@@ -752,20 +753,17 @@ __global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_
   const int32_t* ta = paged_table(a, seq, head);
   const int32_t* tb = paged_table(b, seq, head);
   for (int j = tid; j < p.kept_cols; j += kT) {
-    long long src = -1, dst = 0;
     int s = -1;
     if (j < e.count) {
       s = s_kept[j];
+      int ga = -1, gb = -1, ra = 0, rb = 0;
       if (!(kInPlace && s == j)) {
-        int ra, rb;
-        const int ga = paged_lookup(a, ta, s, ra), gb = paged_lookup(b, tb, j, rb);
-        if (ga >= 0 && gb >= 0) {
-          src = ga * a.page_b + ra * a.slot_b;
-          dst = gb * b.page_b + rb * b.slot_b;
-        }
+        ga = paged_lookup(a, ta, s, ra);
+        gb = paged_lookup(b, tb, j, rb);
       }
-      s_src[j] = src;
-      s_dst[j] = dst;
+      s_from[j] = gb < 0 ? -1 : ga;
+      s_to[j] = gb;
+      s_rows[j] = (uint32_t)ra | (uint32_t)rb << 16;
     }
     e.kept[j] = s;
   }
@@ -777,17 +775,26 @@ __global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_
   for (int j0 = 0; j0 < e.count; j0 += kWarps * kU * kRpi) {
     const int j1 = j0 + warp * kU * kRpi + lane / kL;
     uint4 x[kU];
-    long long src[kU];
+    bool ok[kU];
+    long long at[kU];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int j = j1 + u * kRpi;
-      src[u] = j < e.count ? s_src[j] : -1;
-      if (src[u] >= 0) x[u] = *reinterpret_cast<const uint4*>(from + src[u]);
+    for (int u = 0; u < kU; ++u) {                           // addresses first: loads that wait for none but their own
+      const int j = min(j1 + u * kRpi, e.count - 1), page = s_from[j];
+      ok[u] = j1 + u * kRpi < e.count && page >= 0;
+      at[u] = max(page, 0) * a.page_b + (s_rows[j] & 0xffffu) * a.slot_b;
     }
-    if constexpr (kInPlace) __syncthreads();
 #pragma unroll
     for (int u = 0; u < kU; ++u)
-      if (src[u] >= 0) *reinterpret_cast<uint4*>(to + s_dst[j1 + u * kRpi]) = x[u];
+      if (ok[u]) x[u] = *reinterpret_cast<const uint4*>(from + at[u]);
+    if constexpr (kInPlace) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = min(j1 + u * kRpi, e.count - 1);
+      at[u] = max(s_to[j], 0) * b.page_b + (s_rows[j] >> 16) * b.slot_b;
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (ok[u]) *reinterpret_cast<uint4*>(to + at[u]) = x[u];
   }
   if (a.ks) {                                                // the scales, like the scores, in rounds of four
     for (int j0 = 0; j0 < e.count; j0 += 4 * kT) {
@@ -797,11 +804,10 @@ __global__ void __launch_bounds__(kT) ssd_paged_evict_short_kernel(const __grid_
       for (int u = 0; u < 4; ++u) {
         const int j = j0 + u * kT + tid;
         put[u] = -1;
-        if (j < e.count && s_src[j] >= 0) {
-          int ra, rb;
-          const int ga = paged_lookup(a, ta, s_kept[j], ra), gb = paged_lookup(b, tb, j, rb);
-          const long long at = ga * a.sc_page + head * a.sc_head + ra * a.sc_slot;
-          put[u] = gb * b.sc_page + head * b.sc_head + rb * b.sc_slot;
+        if (j < e.count && s_from[j] >= 0) {
+          const long long ra = s_rows[j] & 0xffffu, rb = s_rows[j] >> 16;
+          const long long at = s_from[j] * a.sc_page + head * a.sc_head + ra * a.sc_slot;
+          put[u] = s_to[j] * b.sc_page + head * b.sc_head + rb * b.sc_slot;
           sk[u] = a.ks[at];
           sv[u] = a.vs[at];
         }
