@@ -26,8 +26,10 @@ cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem,
 }
 
 // ----------------------------------------------------------------------------- append
-// A warp takes four heads of one token (8 rows, K and V): 2 D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads
-// before the first store.  Bound by the bytes of the rows for a chunk of prompts, by latency for one decode step.
+// A warp takes four heads of one token (8 rows, K and V): D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads before the
+// first store, and on their way while the token's sequence is looked for.  Latency for one decode step (64 x 32 heads 2.1
+// us); a chunk of prompts to 8-bit rows is bound by the quantiser's instructions (9142 tokens of 8 heads 18 us = 3.1 TB/s; 24
+// us with divisions and a look-up per head; eight heads per warp 21 us).
 constexpr int kAppendHeads = 4;
 
 struct AppendPagedParams {
@@ -509,7 +511,7 @@ __device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHe
 // The choice among any number of candidates, keys of up to kHeld of them in shared memory (beyond, they are worked out from
 // the scores again every time).  Counts of the keys in 2048 equal bins from the least to the greatest say which bin holds the
 // smallest key to be taken; a bin of few keys is ranked outright, one of many is divided again (at most twice, since 33 bits
-// make three times 11).  A bit at a time, like the short tables, took 44 us for 32768 slots: every step waits for the whole
+// make three times 11).  32768 slots take 27 us; a bit at a time, like the short tables, took 50: every step waits for the whole
 // thread block.
 constexpr int kLongThreads = 1024, kHeld = 32768, kBins = 2048, kFew = 256;
 
@@ -697,7 +699,8 @@ __device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int h
   }
 }
 
-// From the list of ssd_paged_select_kernel.  Elsewhere: a warp per 32 tokens.  In place: a thread block has 64 bytes of every
+// From the list of ssd_paged_select_kernel.  Elsewhere: a warp per 32 tokens (16 x 8 heads, 3 to 4 thousand tokens each of 256
+// bytes with gaps between: 55 us = 4.9 TB/s, after 27 us for the choice).  In place: a thread block has 64 bytes of every
 // row of a head (blockIdx.y), in rounds of 256 tokens: all rows of a round are read before the first is written, and later
 // rounds read only above what it writes.
 template <int kRow, bool kInPlace>
@@ -975,7 +978,8 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   p.scale_log2 = scale * 1.44269504088896340736f;
   p.bf16 = a->q_dtype == SSD_PAGED_BF16;
   // Pieces that one head may be cut into, times query heads: up to 16 a warp joins as it goes (128: a thread block); more
-  // are worth a launch of their own, which spreads them over the GPU (16 query heads x 37 pieces: 62 us against 57 ..).
+  // are worth a launch of their own, which spreads them over the GPU (4 heads of 200001 slots, 16 query heads and 37 pieces
+  // each: 61.5 us without, 59.0 with; 64 x 32 heads, one query head, mostly two pieces: 66.8 us without, 69.0 with).
   const int row_b = kv->head_dim * elem_bytes(kv->dtype), tiles = (int)((p.c.cap * (long long)row_b + 4095) / 4096);
   const int heads = p.c.n_seqs * p.c.H * p.qt;
   // About as many heads as SMs, and none long (64 tiles, eight for every warp): no shares, a thread block per head.  (8 x 16

@@ -22,9 +22,15 @@
 //
 // Products on the tensor cores, transposed: S^T = K Q^T and O^T = V^T P^T, so that the keys and the head dimension
 // fill the 16 rows of an m16n8k16 product and the query heads its 8 columns (kNt = 2: 16 heads).  The work is bound by
-// the bytes of K and V (per 8 KB tile: 24 products and 16 ldmatrix for 8 heads, a fraction of the 8 KB's time on HBM).
+// the bytes of K and V (per 8 KB tile: 24 products and 16 ldmatrix for 8 heads, a fraction of the 8 KB's time on HBM):
+// without the products the same launches take 1 to 3 us less.  Measured: 64 x 32 heads of up to 640 bf16 slots 67 us = 5.8
+// TB/s, of which 5 us pass before the first tile is there and 3 us until the last warp is done; 16 x 8 heads of up to 32768
+// slots, 8 query heads each, 155 us = 6.1 TB/s (reading with torch.sum: 6.2 TB/s).  8-bit rows with 16 query heads are bound
+// by instructions: 4 heads of 200001 slots 50 us = 4.2 TB/s (when it was 61 us, 48 without the products).
+// Boxes of the TMA unit instead of 16-byte copies (swizzled tensor maps, an mbarrier per stage, rows mended after they are
+// there) streamed no faster and began 1 us later: 76 us instead of 72 at 64 x 32 heads.
 // For the second product the weights are a sum of two 16-bit terms, which keeps 16 (bf16) or 22 (fp16) bits of them; over
-// 8-bit rows, whose values have 4 bits, they are one fp16 number each (11 bits; 200001 slots of 4 x 16 heads 59 -> 56 us).
+// 8-bit rows, whose values have 4 bits, they are one fp16 number each (11 bits; 200001 slots of 4 x 16 heads 59 -> 52 us).
 // All sums are in 32 bits.  The weights are held 2^14 times too large (kPagedShift) so that the small
 // ones of a long row stay normal numbers in fp16; the factor is in l too and cancels.
 // 8-bit rows are widened to fp16, which holds every code exactly; q is brought into fp16's range by a power of two per
@@ -38,7 +44,6 @@
 
 namespace ssd {
 namespace paged {
-
 
 // Warps of a thread block (one to an SM) and stages of a warp.  8 x 2 x 8 KB in flight feed 16-bit rows; more make them
 // slower (16 x 8 heads of up to 32768 slots: 8 warps 183 us, 10 192, 12 200; three stages 208), fewer do not keep up.
