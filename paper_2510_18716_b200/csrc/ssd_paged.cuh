@@ -178,7 +178,9 @@ struct PagedDecodeParams {
   int bf16;                 // type of q, out, k_new, v_new: 1 bf16, 0 fp16
 };
 
-enum { kPagedBf16 = 0, kPagedFp16 = 1, kPagedE4m3 = 2 };
+// What the attention kernel is made for: the pages' type, and for 8-bit pages the result's (bf16; fp16: kPagedE4m3Fine)
+enum { kPagedBf16 = 0, kPagedFp16 = 1, kPagedE4m3 = 2, kPagedE4m3Fine = 3 };
+__host__ __device__ constexpr bool paged_8bit(int fmt) { return fmt >= kPagedE4m3; }
 
 // query heads that one pass over a key head's rows serves
 inline int paged_rows(int g) { return g < 16 ? g : 16; }

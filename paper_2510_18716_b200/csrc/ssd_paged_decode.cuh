@@ -30,9 +30,10 @@
 // Boxes of the TMA unit instead of 16-byte copies (swizzled tensor maps, an mbarrier per stage, rows mended after they are
 // there) streamed no faster and began 1 us later: 76 us instead of 72 at 64 x 32 heads.
 // For the second product the weights are a sum of two 16-bit terms, which keeps 16 (bf16) or 22 (fp16) bits of them; over
-// 8-bit rows, whose values have 4 bits, they are one fp16 number each (11 bits; 200001 slots of 4 x 16 heads 59 -> 52 us).
-// All sums are in 32 bits.  The weights are held 2^14 times too large (kPagedShift) so that the small
-// ones of a long row stay normal numbers in fp16; the factor is in l too and cancels.
+// 8-bit rows, with a result in bf16, they are one fp16 number each (11 bits, of which the result shows 8; 200001 slots of 4 x
+// 16 heads 59 -> 50 us).  A result in fp16 would show it, so there they have two terms (53 us).  All sums are in 32 bits.
+// The weights are held 2^14 times too large (kPagedShift) so that the small ones of a long row stay normal numbers in fp16;
+// the factor is in l too and cancels.
 // 8-bit rows are widened to fp16, which holds every code exactly; q is brought into fp16's range by a power of two per
 // head, the K scale multiplies the logit, and the V scale's power of two 2^e is added to it: the running maximum is that
 // of x + e, so that a weight times its V scale is 2^15 at most whatever the scales of other rows; l takes 2^-e back out.
@@ -52,14 +53,14 @@ namespace paged {
 constexpr int kWarps16 = 8, kWarps8 = 12;
 template <int D, int kFmt, int kNt>
 struct Geo {
-  static constexpr int kWarps = kFmt == kPagedE4m3 && kNt == 1 ? kWarps8 : kWarps16;
+  static constexpr int kWarps = paged_8bit(kFmt) && kNt == 1 ? kWarps8 : kWarps16;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = 2;
-  static constexpr int kRow = kFmt == kPagedE4m3 ? D : 2 * D;      // bytes of a row in a page
+  static constexpr int kRow = paged_8bit(kFmt) ? D : 2 * D;       // bytes of a row in a page
   static constexpr int kTile = 4096 / kRow;                        // keys of a tile
   static constexpr int kCpr = kRow / 16;                           // 16-byte chunks of a row
   static constexpr int kRpl = (kTile + 31) / 32;                   // rows of a tile whose address a lane works out
-  static constexpr int kScaleBytes = kFmt == kPagedE4m3 ? kTile * 8 : 0;
+  static constexpr int kScaleBytes = paged_8bit(kFmt) ? kTile * 8 : 0;
   static constexpr int kMaskAt = 8192 + kScaleBytes;               // 2 words: which rows exist
   static constexpr int kStage = (kMaskAt + 8 + 127) / 128 * 128;
   static constexpr int kRing = kStage * kStages;
@@ -147,6 +148,7 @@ template <int D, int kFmt, int kNt>
 struct Worker {
   using G = Geo<D, kFmt, kNt>;
   static constexpr bool kBf16 = kFmt == kPagedBf16;        // type of the products' operands
+  static constexpr int kTerms = kFmt == kPagedE4m3 ? 1 : 2;         // 16-bit terms of a weight
   static constexpr int kKs = D / 16;
   const PagedDecodeParams& p;
   const int lane;
@@ -163,7 +165,7 @@ struct Worker {
 
   // dimension of the O accumulator c[0], c[1] (half 0) or c[2], c[3] (half 1) of product mt
   __device__ __forceinline__ int dim_of(int mt, int half) const {
-    return kFmt == kPagedE4m3 ? 16 * mt + 2 * (lane >> 2) + half : 16 * mt + 8 * half + (lane >> 2);
+    return paged_8bit(kFmt) ? 16 * mt + 2 * (lane >> 2) + half : 16 * mt + 8 * half + (lane >> 2);
   }
 
   __device__ __forceinline__ void begin(int seq, int head, int qi) {
@@ -172,12 +174,12 @@ struct Worker {
     for (int nt = 0; nt < kNt; ++nt) {
       const int h = nt * 8 + (lane >> 2);
       const char* q = p.q + seq * p.q_seq + ((long long)head * p.g + qi * p.rows + h) * p.q_head;
-      const int at = kFmt == kPagedE4m3 ? 8 * (lane & 3) : 4 * (lane & 3);   // bytes; which dimensions is the K side's order
+      const int at = paged_8bit(kFmt) ? 8 * (lane & 3) : 4 * (lane & 3);   // bytes; which dimensions is the K side's order
 #pragma unroll
       for (int ks = 0; ks < kKs; ++ks) {
         uint2 w = make_uint2(0u, 0u);
         if (h < n_q) {
-          if constexpr (kFmt == kPagedE4m3) {
+          if constexpr (paged_8bit(kFmt)) {
             w = *reinterpret_cast<const uint2*>(q + 32 * ks + at);
           } else {
             w.x = *reinterpret_cast<const uint32_t*>(q + 32 * ks + at);
@@ -188,7 +190,7 @@ struct Worker {
         qf[nt][ks][1] = w.y;
       }
       float by = 1.f;
-      if constexpr (kFmt == kPagedE4m3) {
+      if constexpr (paged_8bit(kFmt)) {
         // fp16 copies of q: a power of two brings the head's largest value to [2^11, 2^12), which loses nothing that
         // 24 bits of the products' sum would show (what falls below fp16's smallest step is 2^-36 of the largest)
         float x[kKs][4], top = 0.f;
@@ -227,7 +229,7 @@ struct Worker {
       // the logits' columns of this thread are heads 2 (lane & 3) and the next one
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        cs[nt][e] = p.scale_log2 * (kFmt == kPagedE4m3 ? __shfl_sync(0xffffffffu, by, ((2 * (lane & 3) + e) * 4)) : 1.f);
+        cs[nt][e] = p.scale_log2 * (paged_8bit(kFmt) ? __shfl_sync(0xffffffffu, by, ((2 * (lane & 3) + e) * 4)) : 1.f);
 #pragma unroll
       for (int mt = 0; mt < kKs; ++mt)
 #pragma unroll
@@ -316,7 +318,7 @@ struct Worker {
           k += kRpi * c.slot_b;
         }
       }
-      if constexpr (kFmt == kPagedE4m3) {
+      if constexpr (paged_8bit(kFmt)) {
         const long long so = ok ? page * c.sc_page + head * c.sc_head + row0 * c.sc_slot : 0;
 #pragma unroll
         for (int i = 0; i < G::kRpl; ++i) {
@@ -347,7 +349,7 @@ struct Worker {
       if (held && !ok) paged_flag(c, kPagedBadPage);
       off[i] = ok && !(fused && local == last) ? r.page[i] * c.page_b + head * c.head_b + r.row[i] * c.slot_b : -1;
       have[i] = __ballot_sync(0xffffffffu, ok);
-      if constexpr (kFmt == kPagedE4m3) {
+      if constexpr (paged_8bit(kFmt)) {
         const long long so = ok ? r.page[i] * c.sc_page + head * c.sc_head + r.row[i] * c.sc_slot : 0;
         if (local < G::kTile && !(fused && local == last)) {
           cp4(base + 8192 + local * 4, c.ks + so, ok);
@@ -395,7 +397,7 @@ struct Worker {
     const long long off = ok ? page * c.page_b + head * c.head_b + row * c.slot_b : 0;
     char* to = (lane < 16 ? c.k : c.v) + off;
     const uint32_t sm = base + (lane < 16 ? 0u : 4096u);
-    if constexpr (kFmt == kPagedE4m3) {
+    if constexpr (paged_8bit(kFmt)) {
       float scale;
       const uint2 code = paged_quantize<kL>(raw, p.bf16 != 0, scale);
       if (mine) {
@@ -436,7 +438,7 @@ struct Worker {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[sb][nt][i] = s2[sb][nt][i] = 0.f;
       const int krow = sb * 16 + (mi & 1) * 8 + ml8;         // keys of matrix mi: halves alternate, then chunks
-      if constexpr (kFmt == kPagedE4m3) {
+      if constexpr (paged_8bit(kFmt)) {
 #pragma unroll
         for (int c2 = 0; c2 < kKs / 2; ++c2) {
           uint32_t r[4];
@@ -466,14 +468,14 @@ struct Worker {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {                       // key j8 + 8 hf of the 16
         const bool ok = (word >> (8 * hf)) & 1u;
-        const float kscale = kFmt == kPagedE4m3 ? reinterpret_cast<const float*>(mem + 8192)[sb * 16 + j8 + 8 * hf] : 1.f;
+        const float kscale = paged_8bit(kFmt) ? reinterpret_cast<const float*>(mem + 8192)[sb * 16 + j8 + 8 * hf] : 1.f;
 #pragma unroll
         for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float& x = s[sb][nt][2 * hf + e];
             if (kTwo) x += s2[sb][nt][2 * hf + e];
-            x = ok ? x * (kFmt == kPagedE4m3 ? cs[nt][e] * kscale : cs[nt][e]) : kPagedNegInf;
+            x = ok ? x * (paged_8bit(kFmt) ? cs[nt][e] * kscale : cs[nt][e]) : kPagedNegInf;
           }
       }
     }
@@ -504,7 +506,7 @@ struct Worker {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         float add = 0.f;
-        if constexpr (kFmt == kPagedE4m3) {
+        if constexpr (paged_8bit(kFmt)) {
           // e between bounds that keep l (sums of 2^(14 - e)) and the weights in float32's range; below 2^-100 the scale
           // itself says how small the row is
           const float vs = reinterpret_cast<const float*>(mem + 8192)[G::kTile + sb * 16 + j8 + 8 * hf];
@@ -518,7 +520,7 @@ struct Worker {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float& x = s[sb][nt][2 * hf + e];
-            if constexpr (kFmt == kPagedE4m3) x += add;
+            if constexpr (paged_8bit(kFmt)) x += add;
             top[nt][e] = fmaxf(top[nt][e], x);
           }
       }
@@ -551,14 +553,14 @@ struct Worker {
     }
 #pragma unroll
     for (int sb = 0; sb < kSub; ++sb) {
-      uint32_t bh[kNt][2], bl[kNt][2];
+      uint32_t bh[kNt][2], bl[kNt][2];                       // the weights' two terms, transposed
 #pragma unroll
       for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           float w0 = ex2(s[sb][nt][2 * hf] - (m[nt][0] - kPagedShift));
           float w1 = ex2(s[sb][nt][2 * hf + 1] - (m[nt][1] - kPagedShift));
-          if constexpr (kFmt == kPagedE4m3) {
+          if constexpr (paged_8bit(kFmt)) {
             l[nt][0] = fmaf(w0, vinv[sb][hf], l[nt][0]);
             l[nt][1] = fmaf(w1, vinv[sb][hf], l[nt][1]);
             w0 *= vman[sb][hf];
@@ -570,9 +572,9 @@ struct Worker {
           uint32_t hi, lo;
           split2<kBf16>(w0, w1, hi, lo);
           bh[nt][hf] = transpose8(hi);
-          if constexpr (kFmt != kPagedE4m3) bl[nt][hf] = transpose8(lo);
+          if constexpr (kTerms == 2) bl[nt][hf] = transpose8(lo);
         }
-      if constexpr (kFmt == kPagedE4m3) {
+      if constexpr (paged_8bit(kFmt)) {
         const int vrow = sb * 16 + (mi & 1) * 8 + ml8;
 #pragma unroll
         for (int c2 = 0; c2 < kKs / 2; ++c2) {
@@ -585,6 +587,7 @@ struct Worker {
 #pragma unroll
             for (int nt = 0; nt < kNt; ++nt) {
               mma<kBf16>(o[nt][2 * c2 + u], a, bh[nt]);
+              if constexpr (kTerms == 2) mma<kBf16>(o[nt][2 * c2 + u], a, bl[nt]);
             }
           }
         }

@@ -4,7 +4,9 @@
 namespace ssd {
 
 cudaError_t launch_paged_decode_8(const PagedDecodeParams& p, int head_dim, int sms, cudaStream_t st) {
-  return head_dim == 128 ? paged::launch_paged_format<128, kPagedE4m3>(p, sms, st) : paged::launch_paged_format<64, kPagedE4m3>(p, sms, st);
+  if (p.bf16)
+    return head_dim == 128 ? paged::launch_paged_format<128, kPagedE4m3>(p, sms, st) : paged::launch_paged_format<64, kPagedE4m3>(p, sms, st);
+  return head_dim == 128 ? paged::launch_paged_format<128, kPagedE4m3Fine>(p, sms, st) : paged::launch_paged_format<64, kPagedE4m3Fine>(p, sms, st);
 }
 
 }  // namespace ssd

@@ -4,10 +4,10 @@ Tolerances.  With u = 2^-24, D the head dimension, n the slots, x = scale q.k an
 a logit is a sum of D exact products in float32, each of the D additions off by at most 2^-23 of the partial sums (the
 products' unit truncates): |dx| <= D 2^-23 A, and its scaling and the subtraction of the maximum add 4 u (|x| + |m|),
 both below 8 u A, and 16 u for the constant 2^14 that the weights carry (14 / 2^k steps of u).  e^x adds 2^-22, the two-term
-rounding of a weight 2^-17 (bf16: 2^-9 twice, and a margin of two; fp16 less; over 8-bit pages a weight is one fp16 number,
-whose rounding is off by 2^-11 at most), the sums over n slots at most n u relative to
+rounding of a weight 2^-17 (bf16: 2^-9 twice, and a margin of two; fp16 less; over 8-bit pages, with a bf16 result, a
+weight is one fp16 number, whose rounding is off by 2^-11 at most), the sums over n slots at most n u relative to
 the sum of the absolute terms, merging and the final division 2^-21.  So a weight is off by at most
-    delta = D 2^-23 A + 8 u A + 2^-17 (8 bits: 2^-11) + n u + 2^-20     (relative)
+    delta = D 2^-23 A + 8 u A + 2^-17 (8 bits to bf16: 2^-11) + n u + 2^-20     (relative)
 and twice that after the division by the sum, which has the same error.  In fp16 (fp16 and 8-bit pages) a weight also has an
 absolute error: the largest is held at 2^14, the smallest step is 2^-24, so half a step is 2^-39 of the largest; with a margin
 of two an output is off by 2^-38 max(w) sum |v| on that account (8 bits: 2^-38 max(w scale) sum |code|, the scale being part
@@ -125,7 +125,7 @@ def reference(c, q, scale=None):
             e = (x - m).exp()
             z = e.sum(dim=1, keepdim=True)
             w = e / z
-            delta = c.d * 2.0 ** -23 * a + 8 * U * a + (2.0 ** -11 if c.dtype == "e4m3" else 2.0 ** -17) + n * U + 2.0 ** -20
+            delta = c.d * 2.0 ** -23 * a + 8 * U * a + (2.0 ** -11 if c.dtype == "e4m3" and q.dtype == torch.bfloat16 else 2.0 ** -17) + n * U + 2.0 ** -20
             o = w @ v
             out[i, h * g:(h + 1) * g] = o
             floor = 0.0
