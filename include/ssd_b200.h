@@ -386,7 +386,8 @@ int64_t ssd_debug_decode_plan(int32_t n_heads, const int32_t *head_recs, int32_t
  * whose page number lies outside [0, n_pages) counts as masked and is never written, a length
  * outside [0, max_pages * page_size] is cut to that range, and either sets a bit of *status.  What a
  * call writes (pages of the appended or moved rows, lengths, scores) must not be used by another
- * stream meanwhile.  Row and table strides are not negative; pages and their strides, q, out and the
+ * stream meanwhile, and lies apart: a call that would write through a stride of 0 over more than one
+ * sequence, head, page or slot is refused (the sequences' tables included).  Strides are not negative; pages and their strides, q, out and the
  * new rows are aligned to 16 bytes. */
 enum ssd_paged_dtype { SSD_PAGED_BF16 = 0, SSD_PAGED_FP16 = 1, SSD_PAGED_E4M3 = 2 };
 

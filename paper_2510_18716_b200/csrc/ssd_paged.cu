@@ -890,6 +890,20 @@ int check_view(const ssd_paged_kv* k, PagedView* v) {
   return SSD_OK;
 }
 
+// Whether what a call writes has places of its own: a stride of 0 over more than one of something has not (a tensor's
+// broadcast dimension), and its writes would race.
+bool pages_apart(const ssd_paged_kv* k) {
+  const bool heads = k->n_kv_heads > 1 && k->table_head_stride == 0;        // with a table per head, its pages are its own
+  if ((k->page_stride == 0 && k->n_pages > 1) || (k->slot_stride == 0 && k->page_size > 1) || (k->head_stride == 0 && heads)) return false;
+  if (k->dtype == SSD_PAGED_E4M3 && ((k->scale_page_stride == 0 && k->n_pages > 1) || (k->scale_slot_stride == 0 && k->page_size > 1) ||
+                                     (k->scale_head_stride == 0 && heads)))
+    return false;
+  return k->table_seq_stride != 0 || k->n_seqs <= 1;
+}
+bool scores_apart(const ssd_paged_kv* k) {
+  return !k->scores || !((k->score_seq_stride == 0 && k->n_seqs > 1) || (k->score_head_stride == 0 && k->n_kv_heads > 1));
+}
+
 int sm_count(int* sms) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
@@ -938,6 +952,8 @@ int attend(const ssd_paged_kv* kv, const ssd_paged_attn* a, bool append, void* s
   if (!aligned(a->q, 16) || !aligned(a->out, 16) || (append && (!aligned(a->k_new, 16) || !aligned(a->v_new, 16))) || !aligned(a->lse, 4) ||
       !aligned(a->workspace, 256))
     return SSD_ERR_INVALID_ARG;
+  if ((a->out_seq_stride == 0 && kv->n_seqs > 1) || (a->out_head_stride == 0 && a->n_q_heads > 1)) return SSD_ERR_INVALID_ARG;
+  if ((append && !pages_apart(kv)) || ((append || a->accumulate) && !scores_apart(kv))) return SSD_ERR_INVALID_ARG;
   p.g = a->n_q_heads / kv->n_kv_heads;
   p.rows = paged_rows(p.g);
   p.qt = (p.g + p.rows - 1) / p.rows;
@@ -1034,6 +1050,7 @@ extern "C" int ssd_paged_append(const ssd_paged_kv* kv, const void* k_new, const
   if (new_token_stride < 0 || new_head_stride < 0 || new_token_stride > (int64_t)1 << 48 || new_head_stride > (int64_t)1 << 48 ||
       new_token_stride % 8 != 0 || new_head_stride % 8 != 0 || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(cu_seqlens, 4))
     return SSD_ERR_INVALID_ARG;
+  if (!pages_apart(kv) || !scores_apart(kv)) return SSD_ERR_INVALID_ARG;
   if (n_tokens == 0 || kv->n_seqs == 0) return SSD_OK;
   p.k_new = static_cast<const char*>(k_new);
   p.v_new = static_cast<const char*>(v_new);
@@ -1074,6 +1091,8 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
   } else {
     p.dst = p.src;
   }
+  const ssd_paged_kv* to = into ? into : kv;
+  if (!pages_apart(to) || !scores_apart(to) || (to->len_seq_stride == 0 && to->n_seqs > 1)) return SSD_ERR_INVALID_ARG;
   int64_t most = 0;
   bool same = true;
   for (int h = 0; h < kv->n_kv_heads; ++h) {

@@ -113,6 +113,32 @@ def test_bad_arguments_of_single_calls():
         assert evict(into=kv(**{**other, **c})) == bad
 
 
+def test_writes_through_broadcast_strides_are_refused():
+    """What a call writes needs places of its own; what it only reads may be broadcast (here: up to a later refusal)."""
+    lib, bad = B.load(), B.SSD_ERR_INVALID_ARG
+    ints = (C.c_int32 * 8)(*([4] * 8))
+    other = dict(page_table=AT + 64, lengths=AT + 128, scores=AT + 256)
+    q8 = dict(dtype=2, k_scales=AT, v_scales=AT, scale_page_stride=128, scale_head_stride=16, scale_slot_stride=1)
+    pages = [dict(page_stride=0), dict(head_stride=0), dict(slot_stride=0), dict(table_seq_stride=0)]
+    pages += [{**q8, x: 0} for x in ("scale_page_stride", "scale_head_stride", "scale_slot_stride")]
+    scores = [dict(score_seq_stride=0), dict(score_head_stride=0)]
+    for c in pages + scores:
+        view = kv(**c)
+        assert lib.ssd_paged_append(view, AT, AT, 0, 1024, 128, None, 2, None) == bad
+        assert lib.ssd_paged_append_decode(view, attn(), None) == bad
+        assert lib.ssd_paged_evict(view, None, 4, ints, ints, AT, 12, AT, None) == bad
+        assert lib.ssd_paged_evict(kv(**{k: x for k, x in c.items() if k in q8}), kv(**{**other, **c}), 4, ints, ints, AT, 12, AT, None) == bad
+    for c in scores:
+        assert lib.ssd_paged_decode_attn(kv(**c), attn(accumulate=1), None) == bad
+    assert lib.ssd_paged_evict(kv(len_seq_stride=0), None, 4, ints, ints, AT, 12, AT, None) == bad
+    assert lib.ssd_paged_evict(kv(), kv(**other, len_seq_stride=0), 4, ints, ints, AT, 12, AT, None) == bad
+    for c in (dict(out_seq_stride=0), dict(out_head_stride=0)):
+        assert lib.ssd_paged_decode_attn(kv(), attn(**c), None) == bad
+    # one of something has no stride, a table per head makes its pages the head's own, and an empty step writes nothing
+    one = kv(n_seqs=1, table_seq_stride=0, score_seq_stride=0, table_head_stride=4, head_stride=0)
+    assert lib.ssd_paged_append(one, AT, AT, 0, 1024, 128, AT, 0, None) == B.SSD_OK
+
+
 def test_head_budgets_follow_the_labels():
     b, r = B.head_budgets([1, 0, 0, 1], window=64, sink_budget=96, sink_recent=24)
     assert b == [96, 0, 0, 96] and r == [24, 64, 64, 24]
