@@ -481,7 +481,8 @@ class PagedKV:
 
     The tensors are read when the kernels run: lengths and tables may change between calls, and a captured call
     follows them.  A handle (its workspace) is used on one stream at a time; handles used in turn on one stream may
-    share a workspace (``workspace=other.workspace`` after ``other.reserve``).
+    share a workspace (``workspace=other.workspace`` after ``other.reserve``).  A captured call uses the handle's
+    memory: keep the handle as long as the graph.
     """
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *,
@@ -531,9 +532,12 @@ class PagedKV:
                               ptr(self._status), p[0], p[1], p[2], s[0], s[1], s[2], t[0], t[1] if len(t) > 1 else 0,
                               n[0], n[1] if len(n) > 1 else 0, w[0], w[1], _PAGED_DTYPES[k_pages.dtype], n_seqs, heads, head_dim,
                               page_size, n_pages, page_table.shape[-1], scores.shape[2] if scores is not None else 0)
+        if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
+            raise ValueError("PagedKV: want workspace uint8, contiguous, and zero before its first use")
         self._index = self.device.index
         self._scale = float(softmax_scale)
         self.workspace = workspace
+        self._outgrown = []                                  # workspaces that captured graphs may still use
         self._plan = {}                                      # per call: the arguments last checked, and what goes with them
         self._counts = torch.empty((n_seqs, heads), dtype=torch.int32, device=self.device)
         home = torch.cuda.current_stream(self.device)
@@ -564,6 +568,8 @@ class PagedKV:
             if self.workspace is None or self.workspace.numel() < need + 256:
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("PagedKV: reserve() the workspace before capturing a graph")
+                if self.workspace is not None:
+                    self._outgrown.append(self.workspace)
                 self.workspace = torch.zeros(need + 256, dtype=torch.uint8, device=self.device)
                 torch.cuda.current_stream().synchronize()    # zero before any stream uses it
 

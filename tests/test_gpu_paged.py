@@ -748,6 +748,25 @@ def test_capture_needs_a_reserved_workspace():
     check_attention(c, q, out, lse)
 
 
+def test_a_captured_call_keeps_the_workspace_it_was_captured_with():
+    c = Paged([900, 33, 400], 4, scores=True)
+    q, more, h = new_q(c, 2), new_q(c, 2), c.kv
+    h.reserve(8)
+    small = h.workspace.data_ptr()
+    want = h.decode_attn(q).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = h.decode_attn(q)
+    h.decode_attn(more, accumulate=True)                     # a larger workspace
+    assert h.workspace.data_ptr() != small
+    fresh = [torch.full((n,), 0x55, dtype=torch.uint8, device="cuda") for n in (1 << 16, 1 << 18, 1 << 20, 1 << 22)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(bool((x == 0x55).all()) for x in fresh)
+    with pytest.raises(ValueError, match="workspace"):
+        B.PagedKV(h.k_pages, h.v_pages, h.page_table, h.lengths, workspace=torch.zeros(8, device="cuda"))
+
+
 def test_caches_of_other_shapes_share_a_workspace():
     a, b = Paged([500, 30], 2), Paged([9, 900, 44], 8, d=64, dtype="fp16")
     a.kv.reserve(64)
