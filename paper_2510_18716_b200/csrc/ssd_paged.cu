@@ -511,7 +511,7 @@ __device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHe
 // The choice among any number of candidates, keys of up to kHeld of them in shared memory (beyond, they are worked out from
 // the scores again every time).  Counts of the keys in 2048 equal bins from the least to the greatest say which bin holds the
 // smallest key to be taken; a bin of few keys is ranked outright, one of many is divided again (at most twice, since 33 bits
-// make three times 11).  32768 slots take 27 us; a bit at a time, like the short tables, took 50: every step waits for the whole
+// make three times 11).  32768 slots take 21 us; a bit at a time, like the short tables, took 50: every step waits for the whole
 // thread block.
 constexpr int kLongThreads = 1024, kHeld = 32768, kBins = 2048, kFew = 256;
 
@@ -620,6 +620,32 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
   }
   const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
   const int a = min(nc, warp * seg), b = min(nc, a + seg);
+  if (held && seg > 8 * 32) {
+    // One pass where no tie lies at the border: lane r keeps round r's votes, of which there are at most 32, and writes their
+    // slots.  32768 slots: 4 us less than counting first and voting again; of few rounds (2000 slots) 1 us more, since few lanes
+    // would write.
+    static_assert(kHeld <= 32 * kT, "a round per lane");
+    unsigned votes = 0u;
+#pragma unroll 8
+    for (int r = 0; r < seg / 32; ++r) {
+      const int i = a + r * 32 + lane;
+      const unsigned v = __ballot_sync(0xffffffffu, i < b && s_key[i] >= t);
+      if (lane == r) votes = v;
+    }
+    uint32_t inc = __popc(votes);
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, s);
+      if (lane >= s) inc += y;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    if (__reduce_add_sync(0xffffffffu, s_warp[lane]) == budget) {
+      int32_t* to = out + __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u) + inc - __popc(votes);
+      for (; votes; votes &= votes - 1u) *to++ = p.prefix + a + lane * 32 + __ffs((int)votes) - 1;
+      return;
+    }
+  }
   emit<kT>(t, budget, p.prefix, a, b, seg / 32, [&](int r) {
     const int i = a + r * 32 + lane;
     return i < b ? key_of(i) : 0u;
@@ -636,17 +662,14 @@ __global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __
   const EvictHead e = evict_head(p, pair);
   list_rest<kLongThreads>(p, e, pair, tid);
   if (!e.all && e.budget > 0) choose_long(p, e, s_dynamic, s_dynamic + kHeld, e.kept + p.prefix);
-  if (!e.to) return;
-  __syncthreads();                                           // the list is complete
-  move_scores<kLongThreads>(p, e, e.kept, tid);
 }
 
 // ----------------------------------------------------------------------------- eviction: moving the rows
 // Token j of a head comes from slot kept[j] >= j.  A warp moves kTokens of them: each lane looks one up (source and
-// destination pages) and copies its scales, then kL lanes at a time copy `kL` chunks of 16 bytes of a token, from chunk
+// destination pages) and copies its scales and its score (first), then kL lanes at a time copy `kL` chunks of 16 bytes of a token, from chunk
 // `chunk0` of its K row and V row side by side.  barrier(): between the last read and the first write of eight instructions.
 template <int kRow, int kL, int kTokens, class B>
-__device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int head, int lane, int chunk0, bool scales, bool in_place, int j0, int count,
+__device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int head, int lane, int chunk0, bool first, bool in_place, int j0, int count,
                                             const int32_t* kept, B barrier) {
   constexpr int kCpr = kRow / 16, kRpi = 32 / kL, kIters = kTokens / kRpi, kU = kIters < 8 ? kIters : 8;
   const PagedView& a = p.src;
@@ -658,10 +681,17 @@ __device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int h
   char* to = (is_v ? b.v : b.k) + head * b.head_b + byte;
   const int j = j0 + lane;
   long long src = -1, dst = 0, to_scale = -1;
-  float sk = 0.f, sv = 0.f;
+  const bool scales = first && a.ks;
+  float sk = 0.f, sv = 0.f, score = 0.f;
+  float* to_score = nullptr;
   if (lane < kTokens && j < count) {
     const int s = kept[j];
     if (!(in_place && s == j) && s >= 0 && s < a.cap) {
+      if (first && p.dst_scores) {
+        if (s < a.score_slots) score = paged_scores(a, seq, head)[s];
+        if (j < b.score_slots) to_score = paged_scores(b, seq, head) + j;
+        else paged_flag(b, kPagedBadScores);
+      }
       int ra, rb;
       const int ga = paged_lookup(a, paged_table(a, seq, head), s, ra), gb = paged_lookup(b, paged_table(b, seq, head), j, rb);
       if (ga >= 0 && gb >= 0) {
@@ -697,10 +727,11 @@ __device__ __forceinline__ void move_tokens(const EvictParams& p, int seq, int h
     b.ks[to_scale] = sk;
     b.vs[to_scale] = sv;
   }
+  if (to_score) *to_score = score;
 }
 
 // From the list of ssd_paged_select_kernel.  Elsewhere: a warp per 32 tokens (16 x 8 heads, 3 to 4 thousand tokens each of 256
-// bytes with gaps between: 55 us = 4.9 TB/s, after 27 us for the choice).  In place: a thread block has 64 bytes of every
+// bytes with gaps between: 57 us = 5.4 TB/s, after 21 us for the choice).  In place: a thread block has 64 bytes of every
 // row of a head (blockIdx.y), in rounds of 256 tokens: all rows of a round are read before the first is written, and later
 // rounds read only above what it writes.
 template <int kRow, bool kInPlace>
@@ -717,12 +748,12 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_move_kernel(const __grid_c
   const int32_t* kept = p.kept + (size_t)pair * p.kept_cols;
   const int first = kInPlace ? warp * 32 : (item - pair * chunks) * 32;
   if (first == 0 && blockIdx.y == 0 && lane == 0) p.dst.lens[seq * p.dst.n_seq + head * p.dst.n_head] = count;
-  const bool scales = p.src.ks != nullptr && blockIdx.y == 0;
+  const bool whole = blockIdx.y == 0;                        // the first part of the rows brings scales and scores
   if constexpr (kInPlace) {
     for (int j0 = 0; j0 < count; j0 += 32 * kWarps)
-      move_tokens<kRow, 4, 32>(p, seq, head, lane, (int)blockIdx.y * 4, scales, true, j0 + first, count, kept, [] { __syncthreads(); });
+      move_tokens<kRow, 4, 32>(p, seq, head, lane, (int)blockIdx.y * 4, whole, true, j0 + first, count, kept, [] { __syncthreads(); });
   } else if (first < count) {
-    move_tokens<kRow, kRow / 8, 32>(p, seq, head, lane, 0, scales, false, first, count, kept, [] {});
+    move_tokens<kRow, kRow / 8, 32>(p, seq, head, lane, 0, whole, false, first, count, kept, [] {});
   }
 }
 
