@@ -1,4 +1,6 @@
 // The paged cache: append, accumulation of the weights, eviction, and the host side of its C ABI.
+#include <cooperative_groups.h>
+
 #include <cmath>
 
 #include "ssd_paged.cuh"
@@ -9,20 +11,27 @@ namespace {
 constexpr int kThreads = 256;
 
 template <class P, class... A>
-cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
+cudaError_t launch_clusters(int cluster, void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, more...);
   count_launch();
   return e;
+}
+template <class P, class... A>
+cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, A... more) {
+  return launch_clusters(1, kernel, grid, threads, smem, st, p, more...);
 }
 
 // ----------------------------------------------------------------------------- append
@@ -362,16 +371,15 @@ __device__ __forceinline__ EvictHead evict_head(const EvictParams& p, int pair) 
   e.to = p.dst_scores && !(e.all && p.in_place) ? paged_scores(p.dst, seq, head) : nullptr;
   return e;
 }
-// Everything that is not a choice, by kT threads.
-template <int kT>
-__device__ __forceinline__ void list_rest(const EvictParams& p, const EvictHead& e, int pair, int tid) {
+// Everything that is not a choice, by thread `tid` of `threads`.
+__device__ __forceinline__ void list_rest(const EvictParams& p, const EvictHead& e, int pair, int tid, int threads) {
   if (e.all) {
-    for (int j = tid; j < e.n; j += kT) e.kept[j] = j;
+    for (int j = tid; j < e.n; j += threads) e.kept[j] = j;
   } else {
-    for (int j = tid; j < p.prefix; j += kT) e.kept[j] = j;
-    for (int j = tid; j < e.recent; j += kT) e.kept[p.prefix + e.budget + j] = e.n - e.recent + j;
+    for (int j = tid; j < p.prefix; j += threads) e.kept[j] = j;
+    for (int j = tid; j < e.recent; j += threads) e.kept[p.prefix + e.budget + j] = e.n - e.recent + j;
   }
-  for (int j = e.count + tid; j < p.kept_cols; j += kT) e.kept[j] = -1;
+  for (int j = e.count + tid; j < p.kept_cols; j += threads) e.kept[j] = -1;
   if (tid == 0) {
     p.counts[pair] = e.count;
     if (!e.all && e.budget > 0 && e.n - e.recent > p.src.score_slots) paged_flag(p.src, kPagedBadScores);    // candidates without a score: 0
@@ -508,29 +516,43 @@ __device__ __forceinline__ void choose_short(const EvictParams& p, const EvictHe
   emit<kT>(t, (uint32_t)e.budget, p.prefix, a, b, seg / 32, [&](int r) { return s_key[(warp * kK + r) * 32 + lane]; }, out);
 }
 
-// The choice among any number of candidates, keys of up to kHeld of them in shared memory (beyond, they are worked out from
-// the scores again every time).  Counts of the keys in 2048 equal bins from the least to the greatest say which bin holds the
-// smallest key to be taken; a bin of few keys is ranked outright, one of many is divided again (at most twice, since 33 bits
-// make three times 11).  32768 slots take 21 us; a bit at a time, like the short tables, took 50: every step waits for the whole
+// The choice among any number of candidates, by a cluster of thread blocks that each have a run of them, keys of up to kHeld of
+// it in shared memory (beyond, eight times as many, they are worked out from the scores again every time).  Counts of the keys in 2048 equal bins
+// from the least to the greatest, summed over the cluster, say which bin holds the smallest key to be taken; a bin of few keys
+// is ranked outright, one of many is divided again (at most twice, since 33 bits make three times 11).  128 heads of 32768
+// slots, a thread block each, take 21 us; a bit at a time, like the short tables, took 50: every step waits for the whole
 // thread block.
-constexpr int kLongThreads = 1024, kHeld = 32768, kBins = 2048, kFew = 256;
+constexpr int kLongThreads = 1024, kHeld = 32768, kBins = 2048, kFew = 256, kMaxCluster = 8;
 
+template <bool kCluster>
 __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHead& e, uint32_t* s_key, uint32_t* s_bin, int32_t* out) {
   constexpr int kT = kLongThreads, kW = kT / 32;
   static_assert(kBins == 2 * kT, "two bins a thread");
-  __shared__ uint32_t s_min[kW], s_max[kW], s_warp[kW], s_few[kFew];
+  __shared__ uint32_t s_min[kW], s_max[kW], s_warp[kW], s_few[kFew], s_all[kFew];
   __shared__ uint32_t s_at, s_need, s_in, s_len, s_t;
+  __shared__ uint32_t s_mine[4];                             // of this thread block: least and greatest key, number of keys >= t and > t
+  namespace cg = cooperative_groups;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int n_blocks = kCluster ? (int)cluster.num_blocks() : 1, block = kCluster ? (int)cluster.block_rank() : 0;
+  auto meet = [&] {
+    if (kCluster) cluster.sync();
+    else __syncthreads();
+  };
+  auto theirs = [&](const uint32_t* x, int r) { return kCluster ? (const uint32_t*)cluster.map_shared_rank(const_cast<uint32_t*>(x), r) : x; };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int nc = e.n - e.recent - p.prefix;                  // candidates: more than the budget
-  const int scored = min(nc, p.src.score_slots - p.prefix);
-  const bool held = nc <= kHeld;
-  auto fetch = [&](int i) { return score_key(i < scored ? e.scores[p.prefix + i] : 0.f); };
+  const int all_c = e.n - e.recent - p.prefix;               // candidates: more than the budget
+  const int run = (all_c + n_blocks - 1) / n_blocks, before_c = min(all_c, block * run);
+  const int nc = min(all_c, before_c + run) - before_c;      // this thread block's
+  const int slot0 = p.prefix + before_c;
+  const int scored = min(nc, p.src.score_slots - slot0);
+  const bool held = !kCluster || run <= kHeld;               // one thread block: tables of up to kHeld slots
+  auto fetch = [&](int i) { return score_key(i < scored ? e.scores[slot0 + i] : 0.f); };
   uint32_t lo = 0xffffffffu, hi = 0u;
   if (held) {
     for (int i0 = 0; i0 < nc; i0 += 16 * kT) {
       float x[16];                                           // all loads before the first use
 #pragma unroll
-      for (int u = 0; u < 16; ++u) x[u] = i0 + u * kT + tid < scored ? e.scores[p.prefix + i0 + u * kT + tid] : 0.f;
+      for (int u = 0; u < 16; ++u) x[u] = i0 + u * kT + tid < scored ? e.scores[slot0 + i0 + u * kT + tid] : 0.f;
 #pragma unroll
       for (int u = 0; u < 16; ++u)
         if (i0 + u * kT + tid < nc) {
@@ -555,6 +577,14 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
   __syncthreads();
   lo = __reduce_min_sync(0xffffffffu, s_min[lane]);
   hi = __reduce_max_sync(0xffffffffu, s_max[lane]);
+  if constexpr (kCluster) {
+    if (tid == 0) { s_mine[0] = lo; s_mine[1] = hi; }
+    cluster.sync();
+    for (int r = 0; r < n_blocks; ++r) {
+      lo = min(lo, theirs(s_mine, r)[0]);
+      hi = max(hi, theirs(s_mine, r)[1]);
+    }
+  }
   const uint32_t budget = (uint32_t)e.budget;
   uint32_t need = budget, t = lo;                            // of the keys from lo to hi; those above hi are taken
   for (;;) {
@@ -568,8 +598,16 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
       const uint32_t x = key_of(i);
       if (x >= lo && x <= hi) atomicAdd(s_bin + ((x - lo) >> shift), 1u);
     }
-    __syncthreads();
-    const uint32_t c1 = s_bin[kBins - 1 - 2 * tid], c0 = s_bin[kBins - 2 - 2 * tid];         // from the top
+    meet();
+    uint32_t c1 = 0u, c0 = 0u;                               // two bins, from the top
+#pragma unroll
+    for (int r = 0; r < (kCluster ? kMaxCluster : 1); ++r) {
+      if (r >= n_blocks) continue;
+      const int from = (r + block) & (n_blocks - 1);         // each from another one at a time
+      const uint2 two = *reinterpret_cast<const uint2*>(theirs(s_bin, from) + kBins - 2 - 2 * tid);
+      c1 += two.y;
+      c0 += two.x;
+    }
     uint32_t inc = c1 + c0;
 #pragma unroll
     for (int s = 1; s < 32; s <<= 1) {
@@ -588,7 +626,7 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
       s_need = need - before - c1;
       s_in = c0;
     }
-    __syncthreads();
+    meet();                                                  // the bins have been read, too
     need = s_need;
     const uint32_t in = s_in;
     lo += s_at << shift;
@@ -599,15 +637,25 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
 #pragma unroll 8
       for (int i = tid; i < nc; i += kT) {
         const uint32_t x = key_of(i);
-        if (x >= lo && x <= hi) s_few[atomicAdd(&s_len, 1u)] = x;
+        if (x >= lo && x <= hi) s_few[atomicAdd(&s_len, 1u) & (kFew - 1u)] = x;
       }
-      __syncthreads();
+      meet();
+      if (kCluster && tid < (int)in) {
+        int i = tid, r = 0;
+        for (int n = (int)*theirs(&s_len, 0); i >= n && r < n_blocks - 1; n = (int)*theirs(&s_len, r)) {
+          i -= n;
+          ++r;
+        }
+        s_all[tid] = theirs(s_few, r)[i];
+      }
+      if (kCluster) __syncthreads();
+      const uint32_t* few = kCluster ? s_all : s_few;
       // the need-th largest: as many as need - 1 are above it, or need - 1 lies among its equals
       if (tid < (int)in) {
-        const uint32_t x = s_few[tid];
+        const uint32_t x = few[tid];
         uint32_t above = 0u, from = 0u;
         for (uint32_t i = 0; i < in; ++i) {
-          const uint32_t y = s_few[i];
+          const uint32_t y = few[i];
           above += y > x;
           from += y >= x;
         }
@@ -618,21 +666,29 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
       break;
     }
   }
+  // which of them: the keys above t, and the first ones equal to it
   const int seg = ((nc + kW - 1) / kW + 31) / 32 * 32;
   const int a = min(nc, warp * seg), b = min(nc, a + seg);
-  if (held && seg > 8 * 32) {
-    // One pass where no tie lies at the border: lane r keeps round r's votes, of which there are at most 32, and writes their
-    // slots.  32768 slots: 4 us less than counting first and voting again; of few rounds (2000 slots) 1 us more, since few lanes
+  const bool voted = held && seg > 8 * 32;
+  unsigned votes = 0u;
+  uint32_t inc = 0u, quota = budget;
+  if (voted || kCluster) {
+    // One pass where no tie lies at the border and rounds are few enough: lane r keeps round r's votes and writes their slots.
+    // 32768 slots: 4 us less than counting first and voting again; of few rounds (2000 slots) 1 us more, since few lanes
     // would write.
     static_assert(kHeld <= 32 * kT, "a round per lane");
-    unsigned votes = 0u;
+    if (held) {
 #pragma unroll 8
-    for (int r = 0; r < seg / 32; ++r) {
-      const int i = a + r * 32 + lane;
-      const unsigned v = __ballot_sync(0xffffffffu, i < b && s_key[i] >= t);
-      if (lane == r) votes = v;
+      for (int r = 0; r < seg / 32; ++r) {
+        const int i = a + r * 32 + lane;
+        const unsigned v = __ballot_sync(0xffffffffu, i < b && s_key[i] >= t);
+        if (lane == r) votes = v;
+      }
+      inc = __popc(votes);
+    } else {
+#pragma unroll 8
+      for (int i = a + lane; i < b; i += 32) inc += fetch(i) >= t;
     }
-    uint32_t inc = __popc(votes);
 #pragma unroll
     for (int s = 1; s < 32; s <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, inc, s);
@@ -640,28 +696,64 @@ __device__ __forceinline__ void choose_long(const EvictParams& p, const EvictHea
     }
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
-    if (__reduce_add_sync(0xffffffffu, s_warp[lane]) == budget) {
+    const uint32_t mine = __reduce_add_sync(0xffffffffu, s_warp[lane]);
+    if constexpr (kCluster) {                                // this thread block's part of the budget, and its place in the list
+      if (tid == 0) s_mine[2] = mine;
+      cluster.sync();
+      uint32_t all = 0u, at = 0u;
+      for (int r = 0; r < n_blocks; ++r) {
+        const uint32_t n = theirs(s_mine, r)[2];
+        all += n;
+        at += r < block ? n : 0u;
+      }
+      quota = mine;
+      if (all != budget) {                                   // more are equal than the budget has room for
+        uint32_t n = 0u;
+#pragma unroll 8
+        for (int i = tid; i < nc; i += kT) n += key_of(i) > t;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) s_min[warp] = n;
+        __syncthreads();
+        n = __reduce_add_sync(0xffffffffu, s_min[lane]);
+        if (tid == 0) s_mine[3] = n;
+        cluster.sync();
+        uint32_t above = 0u, above_before = 0u;
+        for (int r = 0; r < n_blocks; ++r) {
+          const uint32_t x = theirs(s_mine, r)[3];
+          above += x;
+          above_before += r < block ? x : 0u;
+        }
+        const uint32_t room = budget - above, equal_before = at - above_before;
+        at = above_before + min(equal_before, room);
+        quota = n + min(mine - n, room - min(equal_before, room));
+      }
+      out += at;
+    }
+    if (voted && mine == quota) {
       int32_t* to = out + __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u) + inc - __popc(votes);
-      for (; votes; votes &= votes - 1u) *to++ = p.prefix + a + lane * 32 + __ffs((int)votes) - 1;
+      for (; votes; votes &= votes - 1u) *to++ = slot0 + a + lane * 32 + __ffs((int)votes) - 1;
       return;
     }
   }
-  emit<kT>(t, budget, p.prefix, a, b, seg / 32, [&](int r) {
+  emit<kT>(t, quota, slot0, a, b, seg / 32, [&](int r) {
     const int i = a + r * 32 + lane;
     return i < b ? key_of(i) : 0u;
   }, out);
 }
 
-// Any table: a thread block per (sequence, head) makes the list.
-__global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __grid_constant__ EvictParams p) {
+// Any table: a cluster of thread blocks per (sequence, head) makes the list.
+template <bool kCluster>
+__global__ void __launch_bounds__(kLongThreads) ssd_paged_select_kernel(const __grid_constant__ EvictParams p, int cluster) {
   extern __shared__ uint32_t s_dynamic[];                    // kHeld keys, kBins counts
-  const int tid = threadIdx.x;
-  const int pair = blockIdx.x;
+  const int pair = kCluster ? (int)blockIdx.x / cluster : (int)blockIdx.x;
   pdl_wait_predecessor();
   pdl_allow_successor();
   const EvictHead e = evict_head(p, pair);
-  list_rest<kLongThreads>(p, e, pair, tid);
-  if (!e.all && e.budget > 0) choose_long(p, e, s_dynamic, s_dynamic + kHeld, e.kept + p.prefix);
+  list_rest(p, e, pair, ((int)blockIdx.x - pair * cluster) * kLongThreads + threadIdx.x, cluster * kLongThreads);
+  if (!e.all && e.budget > 0) {                              // the same for all of a cluster
+    choose_long<kCluster>(p, e, s_dynamic, s_dynamic + kHeld, e.kept + p.prefix);
+    if (kCluster) cooperative_groups::this_cluster().sync(); // nobody's shared memory goes while another reads it
+  }
 }
 
 // ----------------------------------------------------------------------------- eviction: moving the rows
@@ -1159,8 +1251,13 @@ extern "C" int ssd_paged_evict(const ssd_paged_kv* kv, const ssd_paged_kv* into,
                                  : (many ? launch_evict_short<64, 128>(p, pairs, !into, st) : launch_evict_short<64, 256>(p, pairs, !into, st)));
   } else {
     constexpr int kBytes = (kHeld + kBins) * 4;
-    e = cudaFuncSetAttribute(ssd_paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (e == cudaSuccess) e = launch(ssd_paged_select_kernel, dim3(pairs), kLongThreads, kBytes, st, p);
+    // Thread blocks per head: enough to hold all keys (8 heads of 100000 slots: 56 us, 213 with one each).  More cost more in
+    // summing their counts than they save (2 heads of 32768: 18 us with one each, 21 with eight).
+    int cluster = 1;
+    while (cluster < kMaxCluster && p.src.cap > kHeld * cluster) cluster *= 2;
+    auto* select = cluster > 1 ? ssd_paged_select_kernel<true> : ssd_paged_select_kernel<false>;
+    e = cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e == cudaSuccess) e = launch_clusters(cluster, select, dim3(pairs * cluster), kLongThreads, kBytes, st, p, cluster);
     if (e == cudaSuccess) {
       const int chunks = (int)((most + 31) / 32 > 0 ? (most + 31) / 32 : 1);
       const dim3 grid = into ? dim3((unsigned)(((long long)pairs * chunks + kThreads / 32 - 1) / (kThreads / 32))) : dim3(pairs, 2 * row / 64);

@@ -645,6 +645,59 @@ def test_evict_long_rows(n, place):
     check_evict(c, 3, [4000, 2500], [64, 1], None if place == "in place" else targets(c, top=4100))
 
 
+@pytest.mark.parametrize("heads,cap", [(1, 1100), (3, 5000), (2, 40000), (9, 33000), (20, 9000), (40, 6000), (80, 3000), (80, 40000), (3, 100000), (1, 300000), (9, 300000)])
+def test_evict_choice_over_many_thread_blocks(heads, cap):
+    """The list of long tables alone: one to eight thread blocks per head, keys that fit in shared memory and that do not,
+    ties inside a thread block's run and across several, runs without any candidate."""
+    r = np.random.RandomState(heads + cap)
+    x = np.exp(2.0 * r.randn(heads, cap)).astype(np.float32)
+    n = r.randint(cap // 2, cap + 1, size=heads)
+    n[0] = cap
+    budget, recent = r.randint(1, cap // 3, size=heads), r.randint(0, 40, size=heads)
+    for h in range(heads):
+        kind = (h + (cap == 300000)) % 9
+        if kind == 1:
+            x[h] = r.randint(0, 4, size=cap)                         # ties everywhere
+        elif kind == 2:
+            x[h] = 0.25                                              # nothing else
+        elif kind == 3:
+            x[h] = 1.0 + r.randint(0, 3000, size=cap) * 2.0 ** -23   # bins of many keys
+        elif kind == 4:
+            x[h, : cap // 2] = 7.0                                   # the ties in the first thread blocks
+        elif kind == 5:
+            x[h, cap // 3:] = 1e6                                    # and in the last
+        elif kind == 6:
+            x[h] = np.where(r.rand(cap) < 0.98, np.nan, x[h])
+        elif kind == 7:
+            n[h], recent[h] = min(cap, int(budget[h]) + 5 + 3 + 37), 37         # a few more than are kept
+        elif kind == 8:
+            x[h] = np.where(r.rand(cap) < 0.5, -x[h], x[h])
+    page = 64
+    one = torch.zeros((1, 1, page, 64), dtype=torch.bfloat16, device="cuda")     # every slot is in the same page
+    most = int(3 + (budget + recent).max())
+    wide = -(-most // page)
+    pool = torch.zeros((heads * wide, 1, page, 64), dtype=torch.bfloat16, device="cuda")
+    c = B.PagedKV(one, one.clone(), torch.zeros((1, heads, -(-cap // page)), dtype=torch.int32, device="cuda"),
+                  torch.from_numpy(n.astype(np.int32)).cuda()[None], scores=torch.from_numpy(x).cuda()[None])
+    to = B.PagedKV(pool, pool.clone(), torch.arange(heads * wide, dtype=torch.int32, device="cuda").view(1, heads, wide),
+                   torch.full((1, heads), -1, dtype=torch.int32, device="cuda"), scores=torch.full((1, heads, most), -5.0, device="cuda"))
+    kept = c.evict(3, budget.tolist(), recent.tolist(), into=to)[0].cpu().numpy()
+    moved, lens = to.scores[0].cpu().numpy(), to.lengths[0].cpu().numpy()
+    for h in range(heads):
+        k = int(budget[h] + recent[h] + 3)
+        if n[h] <= k:
+            want = np.arange(n[h])
+        else:
+            key = x[h, 3:n[h] - recent[h]].astype(np.float64)
+            order = np.argsort(-np.where(np.isnan(key), -np.inf, key), kind="stable")[: budget[h]]
+            want = np.concatenate([np.arange(3), 3 + np.sort(order), np.arange(n[h] - recent[h], n[h])])
+        assert np.array_equal(kept[h, : len(want)], want), h
+        assert (kept[h, len(want):] == -1).all() and lens[h] == len(want)
+        assert np.array_equal(moved[h, : len(want)], x[h, want], equal_nan=True)
+        assert (moved[h, len(want):] == -5.0).all()
+    assert c.device_status() == 0 and to.device_status() == 0
+
+
 def test_evict_again_and_again():
     """One token appended and one evicted, many times over (the recent slots move down by one each time)."""
     c = Paged(np.full((3, 4), 41), 4, scores=True, room=2)
