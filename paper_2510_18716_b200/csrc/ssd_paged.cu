@@ -37,8 +37,9 @@ cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem,
 // ----------------------------------------------------------------------------- append
 // A warp takes four heads of one token (8 rows, K and V): D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads before the
 // first store, and on their way while the token's sequence is looked for.  Latency for one decode step (64 x 32 heads 2.1
-// us); a chunk of prompts to 8-bit rows is bound by the quantiser's instructions (9142 tokens of 8 heads 18 us = 3.1 TB/s; 24
-// us with divisions and a look-up per head; eight heads per warp 21 us).
+// us); a chunk of prompts to 8-bit rows is bound by the quantiser's instructions (9142 tokens of 8 heads 17 us = 3.4 TB/s; 24
+// us with divisions and a look-up per head, 19 with every lane working out the scales of all its rows; eight heads per warp
+// 18 us, two 19).
 constexpr int kAppendHeads = 4;
 
 struct AppendPagedParams {
@@ -47,12 +48,15 @@ struct AppendPagedParams {
   const char* v_new;
   long long token_b, head_b;       // bytes
   const int32_t* cu;               // or null: token i is the newest of sequence i
-  int n_tokens, bf16;
+  int n_tokens;
 };
 
-template <int D, bool kQ8>
+enum { kAsIs = 0, kQ8Bf16 = 1, kQ8Fp16 = 2 };        // 16-bit pages; 8-bit pages and what the rows arrive in
+
+template <int D, int kHow>
 __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid_constant__ AppendPagedParams p) {
   constexpr int kL = D / 8, kRows = 32 / kL, kIters = 2 * kAppendHeads / kRows;
+  constexpr bool kQ8 = kHow != kAsIs, kBf16 = kHow == kQ8Bf16;
   const PagedView& c = p.c;
   const int lane = threadIdx.x & 31;
   const int groups = (c.H + kAppendHeads - 1) / kAppendHeads;
@@ -109,14 +113,37 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
     if constexpr (kQ8) to_scale = (is_v ? c.vs : c.ks) + page * c.sc_page + head * c.sc_head + row * c.sc_slot;
   };
   if (shared && mine < c.H) place(mine);
+  RowScale rs = {0.f, 0.f, false};
+  bool slow = false;
+  if constexpr (kQ8) {
+    // A lane works out the scale of one of its row group's kIters rows, which one the group's highest bits say: the rows'
+    // largest magnitudes are exchanged so that every lane ends with that of its own row.
+    uint32_t top[kIters];
+#pragma unroll
+    for (int it = 0; it < kIters; ++it) top[it] = paged_top2(raw[it], kBf16);
+    int o = kL / 2;
+#pragma unroll
+    for (int n = kIters / 2; n >= 1; n >>= 1, o >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const bool upper = lane & o;
+        const uint32_t keep = upper ? top[i + n] : top[i], send = upper ? top[i] : top[i + n];
+        top[i] = paged_max2(keep, __shfl_xor_sync(0xffffffffu, send, o), kBf16);
+      }
+#pragma unroll
+    for (; o >= 1; o >>= 1) top[0] = paged_max2(top[0], __shfl_xor_sync(0xffffffffu, top[0], o), kBf16);
+    rs = paged_row_scale(top[0], kBf16);
+    slow = __any_sync(0xffffffffu, rs.slow);
+  }
 #pragma unroll
   for (int it = 0; it < kIters; ++it) {
     const int head = mine + it * kStep;
     if (!shared && head < c.H) place(head);
     const bool ok = found && head < c.H;
     if constexpr (kQ8) {
-      float scale;
-      const uint2 code = paged_quantize<kL>(raw[it], p.bf16 != 0, scale);
+      const int owner = (lane & ~(kL - 1)) | it * (kL / kIters);
+      const float scale = __shfl_sync(0xffffffffu, rs.scale, owner), r = __shfl_sync(0xffffffffu, rs.r, owner);
+      const uint2 code = paged_codes(raw[it], kBf16, scale, r, slow);
       if (ok) {
         *reinterpret_cast<uint2*>(to) = code;
         if (part == 0) *to_scale = scale;
@@ -1181,13 +1208,14 @@ extern "C" int ssd_paged_append(const ssd_paged_kv* kv, const void* k_new, const
   p.head_b = new_head_stride * 2;
   p.cu = cu_seqlens;
   p.n_tokens = n_tokens;
-  p.bf16 = new_dtype == SSD_PAGED_BF16;
   const long long warps = (long long)n_tokens * ((kv->n_kv_heads + kAppendHeads - 1) / kAppendHeads);
   const long long blocks = (warps * 32 + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffffll) return SSD_ERR_LIMIT;
   const bool q8 = kv->dtype == SSD_PAGED_E4M3;
-  auto* kernel = kv->head_dim == 128 ? (q8 ? ssd_paged_append_kernel<128, true> : ssd_paged_append_kernel<128, false>)
-                                     : (q8 ? ssd_paged_append_kernel<64, true> : ssd_paged_append_kernel<64, false>);
+  const bool bf16 = new_dtype == SSD_PAGED_BF16;
+  auto* kernel = kv->head_dim == 128
+                     ? (!q8 ? ssd_paged_append_kernel<128, kAsIs> : bf16 ? ssd_paged_append_kernel<128, kQ8Bf16> : ssd_paged_append_kernel<128, kQ8Fp16>)
+                     : (!q8 ? ssd_paged_append_kernel<64, kAsIs> : bf16 ? ssd_paged_append_kernel<64, kQ8Bf16> : ssd_paged_append_kernel<64, kQ8Fp16>);
   const cudaError_t e = launch<AppendPagedParams>(kernel, dim3((unsigned)blocks), kThreads, 0, static_cast<cudaStream_t>(stream), p);
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA;

@@ -98,41 +98,87 @@ __device__ __forceinline__ uint32_t paged_e4m3x2(float a, float b) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
   return r;
 }
-// A row is held by kLanes consecutive lanes, 8 values each (16-bit, in raw): its codes, and its scale in all of them.
-template <int kLanes>
-__device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, float& scale) {
-  float x[8], m = 0.f;
-  widen8(raw, bf16, x);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));     // a NaN is passed over
-  // not negative, so the bit patterns order like the values
-  uint32_t top = __float_as_uint(m);
-#pragma unroll
-  for (int o = kLanes / 2; o >= 1; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  m = __uint_as_float(top);
+// The largest magnitude of 8 values, two at a time: a pair of 16-bit numbers.  A NaN is passed over.
+__device__ __forceinline__ uint32_t paged_max2(uint32_t a, uint32_t b, bool bf16) {
+  uint32_t r;
+  if (bf16) {
+    __nv_bfloat162 x, y;
+    memcpy(&x, &a, 4);
+    memcpy(&y, &b, 4);
+    x = __hmax2(x, y);
+    memcpy(&r, &x, 4);
+  } else {
+    __half2 x, y;
+    memcpy(&x, &a, 4);
+    memcpy(&y, &b, 4);
+    x = __hmax2(x, y);
+    memcpy(&r, &x, 4);
+  }
+  return r;
+}
+__device__ __forceinline__ uint32_t paged_top2(const uint4& raw, bool bf16) {
+  constexpr uint32_t kAbs = 0x7fff7fffu;
+  return paged_max2(paged_max2(raw.x & kAbs, raw.y & kAbs, bf16), paged_max2(raw.z & kAbs, raw.w & kAbs, bf16), bf16);
+}
+// A row's scale, from the pairs' largest: divisor (1 for a row of zeros) and its reciprocal.
+struct RowScale {
+  float scale, r;
+  bool slow;                // divide
+};
+__device__ __forceinline__ RowScale paged_row_scale(uint32_t top2, bool bf16) {
+  float a, b;
+  if (bf16) {
+    a = __uint_as_float(top2 << 16);
+    b = __uint_as_float(top2 & 0xffff0000u);
+  } else {
+    __half2 h;
+    memcpy(&h, &top2, 4);
+    a = __low2float(h);
+    b = __high2float(h);
+  }
+  const float m = fmaxf(fmaxf(a, b), 0.f);                   // all NaN: 0
   // Quotients, correctly rounded, from the correctly rounded reciprocal of the divisor and one remainder (Markstein, IBM J.
   // Res. Dev. 34, 1990): three operations per value instead of a division.  The theorem leaves out divisors whose significand
   // is all ones, and wants nothing to overflow or underflow; where it does not hold, divide.
-  const bool sane = m > 0x1p-80f && m < 0x1p80f;
+  const bool sane = (m > 0x1p-80f && m < 0x1p80f) || m == 0.f;
   constexpr float r448 = 1.f / 448.f;
   const float y448 = m * r448;
-  scale = sane ? fmaf(fmaf(-y448, 448.f, m), r448, y448) : __fdiv_rn(m, 448.f);
+  RowScale s;
+  s.scale = sane ? fmaf(fmaf(-y448, 448.f, m), r448, y448) : __fdiv_rn(m, 448.f);
+  s.slow = !sane || (__float_as_uint(s.scale) & 0x7fffffu) == 0x7fffffu;
+  s.r = __frcp_rn(s.scale > 0.f ? s.scale : 1.f);
+  return s;
+}
+__device__ __forceinline__ uint2 paged_codes(const uint4& raw, bool bf16, float scale, float r, bool slow) {
   const float by = scale > 0.f ? scale : 1.f;
-  const float r = __frcp_rn(by);
-  float q[8];
+  float x[8], q[8];
+  widen8(raw, bf16, x);
+  if (!slow) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = x[i] * r;
-    q[i] = copysignf(fmaf(fmaf(-y, by, x[i]), r, y), x[i]);  // the sign of a zero is lost on the way
-  }
-  if (!sane || (__float_as_uint(by) & 0x7fffffu) == 0x7fffffu) {
+    for (int i = 0; i < 8; ++i) {
+      const float y = x[i] * r;
+      q[i] = fmaf(fmaf(-y, by, x[i]), r, y);
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(x[i], by);
   }
   uint32_t c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) c[i] = paged_e4m3x2(q[2 * i], q[2 * i + 1]);
-  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+  // a quotient of -0 has lost its sign on the way
+  constexpr uint32_t kSigns = 0x80808080u;
+  return make_uint2(c[0] | (c[1] << 16) | (__byte_perm(raw.x, raw.y, 0x7531) & kSigns), c[2] | (c[3] << 16) | (__byte_perm(raw.z, raw.w, 0x7531) & kSigns));
+}
+// A row is held by kLanes consecutive lanes, 8 values each (16-bit, in raw): its codes, and its scale in all of them.
+template <int kLanes>
+__device__ __forceinline__ uint2 paged_quantize(const uint4& raw, bool bf16, float& scale) {
+  uint32_t top = paged_top2(raw, bf16);
+#pragma unroll
+  for (int o = kLanes / 2; o >= 1; o >>= 1) top = paged_max2(top, __shfl_xor_sync(0xffffffffu, top, o), bf16);
+  const RowScale s = paged_row_scale(top, bf16);
+  scale = s.scale;
+  return paged_codes(raw, bf16, s.scale, s.r, s.slow);
 }
 #endif
 
