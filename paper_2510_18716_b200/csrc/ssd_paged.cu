@@ -36,7 +36,7 @@ cudaError_t launch(void (*kernel)(P, A...), dim3 grid, int threads, size_t smem,
 
 // ----------------------------------------------------------------------------- append
 // A warp takes four heads of one token (8 rows, K and V): D / 8 = 8 or 16 lanes per row, 16 bytes each, all loads before the
-// first store, and on their way while the token's sequence is looked for.  Latency for one decode step (64 x 32 heads 2.1
+// first store, and on their way while the token's sequence is looked for.  Latency for one decode step (64 x 32 heads 1.9
 // us); a chunk of prompts to 8-bit rows is bound by the quantiser's instructions (9142 tokens of 8 heads 17 us = 3.4 TB/s; 24
 // us with divisions and a look-up per head, 19 with every lane working out the scales of all its rows; eight heads per warp
 // 18 us, two 19).
@@ -59,12 +59,12 @@ __global__ void __launch_bounds__(kThreads) ssd_paged_append_kernel(const __grid
   constexpr bool kQ8 = kHow != kAsIs, kBf16 = kHow == kQ8Bf16;
   const PagedView& c = p.c;
   const int lane = threadIdx.x & 31;
-  const int groups = (c.H + kAppendHeads - 1) / kAppendHeads;
-  const long long item = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
+  // a thread block has the same heads of eight tokens
+  const uint32_t groups = (uint32_t)(c.H + kAppendHeads - 1) / kAppendHeads, eight = blockIdx.x / groups;
+  const int token = (int)(eight * (kThreads / 32) + threadIdx.x / 32), head0 = (int)(blockIdx.x - eight * groups) * kAppendHeads;
   pdl_wait_predecessor();
   pdl_allow_successor();
-  const int token = (int)(item / groups), head0 = (int)(item % groups) * kAppendHeads;
-  if (token >= p.n_tokens) return;
+  if ((uint32_t)token >= (uint32_t)p.n_tokens) return;
   // this lane's rows: head mine + it * kStep, all K or all V
   constexpr int kStep = kRows / 2;
   const int sub = lane / kL, part = lane % kL, mine = head0 + (sub >> 1);
@@ -1208,8 +1208,7 @@ extern "C" int ssd_paged_append(const ssd_paged_kv* kv, const void* k_new, const
   p.head_b = new_head_stride * 2;
   p.cu = cu_seqlens;
   p.n_tokens = n_tokens;
-  const long long warps = (long long)n_tokens * ((kv->n_kv_heads + kAppendHeads - 1) / kAppendHeads);
-  const long long blocks = (warps * 32 + kThreads - 1) / kThreads;
+  const long long blocks = ((long long)n_tokens + kThreads / 32 - 1) / (kThreads / 32) * ((kv->n_kv_heads + kAppendHeads - 1) / kAppendHeads);
   if (blocks > 0x7fffffffll) return SSD_ERR_LIMIT;
   const bool q8 = kv->dtype == SSD_PAGED_E4M3;
   const bool bf16 = new_dtype == SSD_PAGED_BF16;
