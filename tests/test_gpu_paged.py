@@ -762,7 +762,7 @@ def test_captured_step_follows_lengths_and_pages():
     assert bool(((out.double() - want).abs() <= e_out).all())
 
 
-@pytest.mark.parametrize("cap", [64, 2048])
+@pytest.mark.parametrize("cap", [64, 2048, 36000])
 def test_captured_refresh(cap):
     """Append, attention with weights and eviction in one captured graph, replayed: the same bits as the calls one by one."""
     made = [Paged([50, 20, 0, 61], 4, dtype="e4m3", scores=True, room=cap - 61) for _ in range(2)]
